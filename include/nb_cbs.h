@@ -54,9 +54,9 @@
 extern "C" {
 #endif
 
-#define NB_CBS_ABI_VERSION 4u /* 2: adds the evaluation-mode / plain calls (additive); 3: flag 2 is NB_CBS_FLAG_SEPARATE_FINALIZE,
+#define NB_CBS_ABI_VERSION 5u /* 2: adds the evaluation-mode / plain calls (additive); 3: flag 2 is NB_CBS_FLAG_SEPARATE_FINALIZE,
                                   the grid-barrier test hook is gone with the barriers, nb_cbs_plan_set_bwd_residual is new;
-                                  4: adds nb_conv_bn_silu_bwd (additive) */
+                                  4: adds nb_conv_bn_silu_bwd (additive); 5: adds nb_adamw.h, nb_norm.h and nb_linear.h (additive) */
 
 typedef int32_t nb_status;
 enum {

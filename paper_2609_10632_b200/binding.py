@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes
 import itertools
 import os
-from ctypes import POINTER, Structure, byref, c_char_p, c_float, c_int, c_int32, c_size_t, c_uint32, c_void_p
+from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("NB_CBS_LIBRARY") or os.path.join(HERE, "libnb_cbs.so")  # (the variable: another build of the same library, for A/B timing)
@@ -31,6 +31,7 @@ EXPORTS = (
     "nb_bn_fold", "nb_sgd_plan_create", "nb_sgd_plan_destroy", "nb_sgd_workspace_bytes", "nb_sgd_upload", "nb_sgd_clip_nesterov_step", "nb_sgd_clip_nesterov_step_scaled",
     "nb_slice_add", "nb_maxpool5_fwd", "nb_maxpool5_bwd", "nb_upsample2", "nb_conv_bias_bwd", "nb_cbs_plan_set_pitches",
     "nb_cbs_plan_set_dx_target", "nb_cbs_plan_set_fwd_residual", "nb_cbs_plan_set_bwd_residual",
+    "nb_adamw_plan_create", "nb_adamw_plan_destroy", "nb_adamw_workspace_bytes", "nb_adamw_upload", "nb_adamw_step", "nb_adamw_step_scaled",
 )
 
 
@@ -53,6 +54,17 @@ class nb_sgd_hyper(Structure):
 
 class nb_scaler_hyper(Structure):
     _fields_ = [("struct_size", c_uint32), ("growth_factor", c_float), ("backoff_factor", c_float), ("floor_scale", c_float), ("growth_interval", c_int32)]
+
+
+class nb_adamw_tensor(Structure):
+    _fields_ = [("grad", c_void_p), ("param", c_void_p), ("exp_avg", c_void_p), ("exp_avg_sq", c_void_p), ("exp_avg_scale", c_void_p),
+                ("exp_avg_sq_scale", c_void_p), ("param_copy", c_void_p), ("numel", c_int64), ("group", c_int32), ("copy_dtype", c_int32),
+                ("grad_dtype", c_int32), ("state_bits", c_int32)]
+
+
+class nb_adamw_hyper(Structure):
+    _fields_ = [("struct_size", c_uint32), ("eps", c_float), ("max_norm", c_float), ("lr", c_float * 3), ("weight_decay", c_float * 3),
+                ("beta1", c_double), ("beta2", c_double)]
 
 
 class NbError(RuntimeError):
@@ -106,6 +118,12 @@ def load() -> ctypes.CDLL:
         lib.nb_sgd_upload.argtypes = [V, V, c_size_t, V]
         lib.nb_sgd_clip_nesterov_step.argtypes = [V, V, c_size_t, POINTER(nb_sgd_hyper), FP, V]
         lib.nb_sgd_clip_nesterov_step_scaled.argtypes = [V, V, c_size_t, POINTER(nb_sgd_hyper), POINTER(nb_scaler_hyper), V, FP, V]
+        lib.nb_adamw_plan_create.argtypes = [POINTER(nb_adamw_tensor), c_int32, c_int, POINTER(V)]
+        lib.nb_adamw_plan_destroy.argtypes = [V]
+        lib.nb_adamw_workspace_bytes.argtypes = [V, POINTER(c_size_t)]
+        lib.nb_adamw_upload.argtypes = [V, V, c_size_t, V]
+        lib.nb_adamw_step.argtypes = [V, V, c_size_t, POINTER(nb_adamw_hyper), V, FP, V]
+        lib.nb_adamw_step_scaled.argtypes = [V, V, c_size_t, POINTER(nb_adamw_hyper), POINTER(nb_scaler_hyper), V, V, FP, V]
         lib.nb_slice_add.argtypes = [c_int32, ctypes.c_int64, c_int32, V, ctypes.c_int64, V, ctypes.c_int64, V, ctypes.c_int64, c_int32, V]
         lib.nb_maxpool5_fwd.argtypes = [c_int32, c_int32, c_int32, c_int32, c_int32, V, V, V, ctypes.c_int64, ctypes.c_int64, V]
         lib.nb_maxpool5_bwd.argtypes = [c_int32, c_int32, c_int32, c_int32, c_int32, V, V, V, c_int32, ctypes.c_int64, ctypes.c_int64, V]
@@ -167,6 +185,19 @@ def _stream(stream):
             _raw_stream, _raw_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         return _raw_stream(_raw_device())
     return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _stream_on(stream, device):
+    """As _stream, with the current stream of `device` (an ordinal) where `stream` is None."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(device)
+    if stream is None:
+        _stream(None)
+        return _raw_stream(device)
+    return _stream(stream)
+
+
+_TORCH_DTYPES = {"torch.float32": NB_DTYPE_F32, "torch.bfloat16": NB_DTYPE_BF16, "torch.float16": NB_DTYPE_F16}
 
 
 def nb_abi_version() -> int:
@@ -408,6 +439,80 @@ class SgdPlan:
     def close(self):
         if self.handle:
             load().nb_sgd_plan_destroy(self.handle)
+            self.handle = c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _refuse(message, status=NB_ERR_INVALID_ARG):
+    raise NbError(status, message)
+
+
+class AdamWPlan:
+    """Owner of one nb_adamw_plan handle.  `tensors`: iterable of (grad, param, exp_avg, exp_avg_sq, param_copy or None, group) of
+    contiguous device tensors, with (exp_avg_scale, exp_avg_sq_scale) behind them where the moments are held in 8 bits
+    (torch.float8_e4m3fn or torch.uint8, one fp32 scale for each 128 elements)."""
+
+    def __init__(self, tensors, device=0):
+        items = [tuple(it) for it in tensors]
+        arr = (nb_adamw_tensor * max(len(items), 1))()
+        for i, it in enumerate(items):
+            if len(it) not in (6, 8):
+                _refuse(f"tensor {i}: {len(it)} items, 6 or 8 expected")
+            grad, param, m, v, copy, group = it[:6]
+            scales = it[6:] or (None, None)
+            n = param.numel()
+            bits = 8 if str(m.dtype) in ("torch.float8_e4m3fn", "torch.uint8") else 32
+            blocks = -(-n // 128)
+            moment = ("torch.float8_e4m3fn", "torch.uint8") if bits == 8 else ("torch.float32",)
+            for name, t, count, dtypes in (("grad", grad, n, tuple(_TORCH_DTYPES)), ("param", param, n, ("torch.float32",)), ("exp_avg", m, n, moment),
+                                           ("exp_avg_sq", v, n, moment), ("param_copy", copy, n, ("torch.bfloat16", "torch.float16")),
+                                           ("exp_avg_scale", scales[0], blocks, ("torch.float32",)), ("exp_avg_sq_scale", scales[1], blocks, ("torch.float32",))):
+                if t is not None and (str(t.dtype) not in dtypes or t.numel() != count or not t.is_contiguous() or t.device.type != "cuda" or t.device.index != device):
+                    _refuse(f"tensor {i}: {name} must be {count} contiguous elements of {' or '.join(dtypes)} on cuda:{device}")
+            arr[i] = nb_adamw_tensor(_ptr(grad), _ptr(param), _ptr(m), _ptr(v), _ptr(scales[0]), _ptr(scales[1]), _ptr(copy), n, int(group),
+                                     0 if copy is None else _TORCH_DTYPES[str(copy.dtype)], _TORCH_DTYPES[str(grad.dtype)], bits)
+        self.count, self.device = len(items), device
+        self._hyper = self._scaler = (None, None)  # (values, structure) of the last step: they seldom change
+        self.handle = c_void_p()
+        _check(load().nb_adamw_plan_create(arr, self.count, device, byref(self.handle)))
+        b = c_size_t()
+        _check(load().nb_adamw_workspace_bytes(self.handle, byref(b)))
+        self.workspace_bytes = b.value
+
+    def upload(self, workspace, stream=None):
+        _check(load().nb_adamw_upload(self.handle, _ptr(workspace), _nbytes(workspace), _stream_on(stream, self.device)))
+
+    def _hyper_struct(self, lr, weight_decay, beta1, beta2, eps, max_norm):
+        values = (*lr, *weight_decay, beta1, beta2, eps, max_norm)
+        if self._hyper[0] != values:
+            h = nb_adamw_hyper(ctypes.sizeof(nb_adamw_hyper), eps, max_norm, (c_float * 3)(*lr), (c_float * 3)(*weight_decay), beta1, beta2)
+            self._hyper = values, h, byref(h)
+        return self._hyper[2]
+
+    def step(self, workspace, step, lr, weight_decay, beta1, beta2, eps, max_norm, total_norm=None, stream=None):
+        """`step`: a device int64, the steps taken so far (0 before the first); max_norm 0 disables clipping."""
+        h = self._hyper_struct(lr, weight_decay, beta1, beta2, eps, max_norm)
+        _check(load().nb_adamw_step(self.handle, _ptr(workspace), _nbytes(workspace), h, _ptr(step), _ptr(total_norm), _stream_on(stream, self.device)))
+
+    def step_scaled(self, workspace, state, step, lr, weight_decay, beta1, beta2, eps, max_norm, growth_factor=2.0, backoff_factor=0.5, floor_scale=0.0,
+                    growth_interval=2000, total_norm=None, stream=None):
+        """`state`: a 16-byte device buffer laid out as nb_loss_scaler, as in SgdPlan.step_scaled."""
+        h = self._hyper_struct(lr, weight_decay, beta1, beta2, eps, max_norm)
+        values = (growth_factor, backoff_factor, floor_scale, growth_interval)
+        if self._scaler[0] != values:
+            sc = nb_scaler_hyper(ctypes.sizeof(nb_scaler_hyper), growth_factor, backoff_factor, floor_scale, growth_interval)
+            self._scaler = values, sc, byref(sc)
+        _check(load().nb_adamw_step_scaled(self.handle, _ptr(workspace), _nbytes(workspace), h, self._scaler[2], _ptr(state), _ptr(step), _ptr(total_norm),
+                                           _stream_on(stream, self.device)))
+
+    def close(self):
+        if self.handle:
+            load().nb_adamw_plan_destroy(self.handle)
             self.handle = c_void_p()
 
     def __del__(self):
