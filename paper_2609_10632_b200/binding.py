@@ -32,6 +32,7 @@ EXPORTS = (
     "nb_slice_add", "nb_maxpool5_fwd", "nb_maxpool5_bwd", "nb_upsample2", "nb_conv_bias_bwd", "nb_cbs_plan_set_pitches",
     "nb_cbs_plan_set_dx_target", "nb_cbs_plan_set_fwd_residual", "nb_cbs_plan_set_bwd_residual",
     "nb_adamw_plan_create", "nb_adamw_plan_destroy", "nb_adamw_workspace_bytes", "nb_adamw_upload", "nb_adamw_step", "nb_adamw_step_scaled",
+    "nb_layer_norm_fwd", "nb_layer_norm_workspace_bytes", "nb_layer_norm_bwd",
 )
 
 
@@ -124,6 +125,9 @@ def load() -> ctypes.CDLL:
         lib.nb_adamw_upload.argtypes = [V, V, c_size_t, V]
         lib.nb_adamw_step.argtypes = [V, V, c_size_t, POINTER(nb_adamw_hyper), V, FP, V]
         lib.nb_adamw_step_scaled.argtypes = [V, V, c_size_t, POINTER(nb_adamw_hyper), POINTER(nb_scaler_hyper), V, V, FP, V]
+        lib.nb_layer_norm_fwd.argtypes = [c_int32, c_int64, c_int32, V, c_int64, FP, FP, c_float, V, c_int64, FP, FP, V]
+        lib.nb_layer_norm_workspace_bytes.argtypes = [c_int64, c_int32, POINTER(c_size_t)]
+        lib.nb_layer_norm_bwd.argtypes = [c_int32, c_int64, c_int32, V, c_int64, V, c_int64, FP, FP, FP, V, c_int64, V, c_int64, FP, FP, V, c_size_t, V]
         lib.nb_slice_add.argtypes = [c_int32, ctypes.c_int64, c_int32, V, ctypes.c_int64, V, ctypes.c_int64, V, ctypes.c_int64, c_int32, V]
         lib.nb_maxpool5_fwd.argtypes = [c_int32, c_int32, c_int32, c_int32, c_int32, V, V, V, ctypes.c_int64, ctypes.c_int64, V]
         lib.nb_maxpool5_bwd.argtypes = [c_int32, c_int32, c_int32, c_int32, c_int32, V, V, V, c_int32, ctypes.c_int64, ctypes.c_int64, V]
@@ -389,6 +393,25 @@ def nb_upsample2(dtype, n, h, w, c, src, dst, backward=False, accumulate=False, 
     """2x nearest-neighbour upsampling (or its gradient); n, h, w, c and ld_small describe the SMALL tensor, ld_large the large one (pixel pitches, 0 = dense)."""
     _check(load().nb_upsample2(int(dtype), n, h, w, c, _ptr(src), _ptr(dst), 1 if backward else 0, 1 if accumulate else 0, int(ld_small), int(ld_large),
                                _stream(stream)))
+
+
+def nb_layer_norm_fwd(dtype, rows, c, x, gamma, beta, eps, y, mean=None, rstd=None, ld_x=0, ld_y=0, stream=None):
+    """Layer norm over the c channels of each row; mean and rstd (fp32 [rows]) are what the backward call needs."""
+    _check(load().nb_layer_norm_fwd(int(dtype), int(rows), int(c), _ptr(x), int(ld_x), _ptr(gamma), _ptr(beta), float(eps), _ptr(y), int(ld_y), _ptr(mean),
+                                    _ptr(rstd), _stream(stream)))
+
+
+def nb_layer_norm_workspace_bytes(rows, c) -> int:
+    b = c_size_t()
+    _check(load().nb_layer_norm_workspace_bytes(int(rows), int(c), byref(b)))
+    return b.value
+
+
+def nb_layer_norm_bwd(dtype, rows, c, g, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, workspace=None, add=None, ld_g=0, ld_x=0, ld_add=0, ld_dx=0,
+                      stream=None):
+    """dx (plus `add`, the gradient of another branch), and dgamma, dbeta where they are given (then with a workspace)."""
+    _check(load().nb_layer_norm_bwd(int(dtype), int(rows), int(c), _ptr(g), int(ld_g), _ptr(x), int(ld_x), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(add),
+                                    int(ld_add), _ptr(dx), int(ld_dx), _ptr(dgamma), _ptr(dbeta), _ptr(workspace), _nbytes(workspace), _stream(stream)))
 
 
 class SgdPlan:
