@@ -77,7 +77,7 @@ template <typename T> nb_status run_fwd(LnFwd P, bool vec, cudaStream_t st) {
 // Blocks of the backward call, each of which leaves a row of partial sums: as many as are resident, fewer where rows are long and
 // the partial sums would be read and written for longer than they help.
 int bwd_blocks(long long rows, int c, int sms) {
-    const long long most = (long long)sms * (c <= 1024 ? 6 : c <= 4096 ? 4 : 2);
+    const long long most = (long long)sms * (c <= 1024 ? 6 : c <= 2048 ? 4 : 2);
     return (int)std::max<long long>(1, std::min(rows, most));
 }
 
@@ -127,7 +127,7 @@ template <typename T> nb_status run_bwd(LnBwd P, bool vec, int blocks, float* dg
     }
     NB_LAUNCH_OK("layer_norm_bwd");
     if (P.partials) {
-        launch_k(layer_norm_reduce_kernel, dim3((unsigned)((2 * (long long)P.c + 31) / 32)), dim3(1024), 0, st, 1, (const float*)P.partials, parts, P.c, dgamma, dbeta);
+        launch_k(layer_norm_reduce_kernel, dim3((unsigned)((2 * (long long)P.c + LN_RED_COLS - 1) / LN_RED_COLS)), dim3(LN_RED_COLS * LN_RED_ROWS), 0, st, 1, (const float*)P.partials, parts, P.c, dgamma, dbeta);
         NB_LAUNCH_OK("layer_norm_reduce");
     }
     return NB_OK;

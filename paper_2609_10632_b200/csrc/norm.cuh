@@ -27,17 +27,42 @@ template <typename T, int V> __device__ __forceinline__ LnVec<T, V> ln_ld(const 
 template <typename T, int V> __device__ __forceinline__ void ln_st(T* p, const LnVec<T, V>& r) {
     if constexpr (V == 1) *p = r.v[0]; else *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(&r);
 }
-template <int V> __device__ __forceinline__ void ln_ldf(const float* p, float (&o)[V], float without) {
+// The same as packed fp32 pairs (fma / mul / add .f32x2, see common.cuh); a single element is a pair whose second half is zero.
+template <typename T, int V> struct LnPairs {
+    static constexpr int N = (V + 1) / 2;
+    float2 p[N];
+    __device__ __forceinline__ LnPairs() {}
+    __device__ __forceinline__ explicit LnPairs(const LnVec<T, V>& v) {
+        if constexpr (V == 1) {
+            p[0] = make_float2(to_f32<T>(v.v[0]), 0.f);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) p[j] = pair_to_f32<T>(v.v + 2 * j);
+        }
+    }
+    __device__ __forceinline__ LnVec<T, V> rounded() const {
+        LnVec<T, V> o;
+        if constexpr (V == 1) {
+            o.v[0] = from_f32<T>(p[0].x);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) pair_from_f32<T>(o.v + 2 * j, p[j]);
+        }
+        return o;
+    }
+};
+template <int V> __device__ __forceinline__ void ln_ldf(const float* p, float2 (&o)[(V + 1) / 2], float without) {
     if (!p) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) o[j] = without;
+        for (int j = 0; j < (V + 1) / 2; ++j) o[j] = make_float2(without, without);
     } else if constexpr (V == 1) {
-        o[0] = __ldg(p);
+        o[0] = make_float2(__ldg(p), 0.f);
     } else {
 #pragma unroll
         for (int j = 0; j < V; j += 4) {
             const float4 f = __ldg(reinterpret_cast<const float4*>(p + j));
-            o[j] = f.x; o[j + 1] = f.y; o[j + 2] = f.z; o[j + 3] = f.w;
+            o[j / 2] = make_float2(f.x, f.y);
+            o[j / 2 + 1] = make_float2(f.z, f.w);
         }
     }
 }
@@ -89,48 +114,49 @@ template <typename T, int V, int L, int VPL> __global__ void __launch_bounds__(L
         const long long row = r0 + group;
         const bool live = row < P.rows;
         const T* x = static_cast<const T*>(P.x) + (live ? row : 0) * P.ld_x;
-        float f[VPL][V];
-        float s = 0.f;
+        constexpr int N = (V + 1) / 2;
+        LnPairs<T, V> f[VPL];
+        LnVec<T, V> raw[VPL];
 #pragma unroll
         for (int k = 0; k < VPL; ++k) {
             const int i = lane + k * W;
             if (live && i < P.nvec) {
-                const LnVec<T, V> v = ln_ld<T, V>(x + (long long)i * V);
-#pragma unroll
-                for (int j = 0; j < V; ++j) f[k][j] = to_f32<T>(v.v[j]);
+                raw[k] = ln_ld<T, V>(x + (long long)i * V);
             } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j) f[k][j] = 0.f;
+                for (int j = 0; j < V; ++j) raw[k].v[j] = from_f32<T>(0.f);
             }
         }
+        float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < VPL; ++k)
+        for (int k = 0; k < VPL; ++k) {
+            f[k] = LnPairs<T, V>(raw[k]);
 #pragma unroll
-            for (int j = 0; j < V; ++j) s += f[k][j];
-        const float mean = ln_sum<L>(s, red[0]) * inv_c;
-        s = 0.f;
+            for (int j = 0; j < N; ++j) s2 = add2(s2, f[k].p[j]);
+        }
+        const float mean = ln_sum<L>(s2.x + s2.y, red[0]) * inv_c;
+        s2 = make_float2(0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < VPL; ++k)
             if (lane + k * W < P.nvec)
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    f[k][j] -= mean;
-                    s = fmaf(f[k][j], f[k][j], s);
+                for (int j = 0; j < N; ++j) {
+                    f[k].p[j] = add2(f[k].p[j], make_float2(-mean, V == 1 ? 0.f : -mean));
+                    s2 = fma2(f[k].p[j], f[k].p[j], s2);
                 }
-        const float rstd = 1.f / sqrtf(ln_sum<L>(s, red[1]) * inv_c + P.eps);
+        const float rstd = 1.f / sqrtf(ln_sum<L>(s2.x + s2.y, red[1]) * inv_c + P.eps);
         if (!live) continue;
         T* y = static_cast<T*>(P.y) + row * P.ld_y;
 #pragma unroll
         for (int k = 0; k < VPL; ++k) {
             const int i = lane + k * W;
             if (i < P.nvec) {
-                float ga[V], be[V];
+                float2 ga[N], be[N];
                 ln_ldf<V>(P.gamma ? P.gamma + i * V : nullptr, ga, 1.f);
                 ln_ldf<V>(P.beta ? P.beta + i * V : nullptr, be, 0.f);
-                LnVec<T, V> o;
 #pragma unroll
-                for (int j = 0; j < V; ++j) o.v[j] = from_f32<T>(fmaf(f[k][j] * rstd, ga[j], be[j]));
-                ln_st<T, V>(y + (long long)i * V, o);
+                for (int j = 0; j < N; ++j) f[k].p[j] = fma2(mul2(f[k].p[j], splat2(rstd)), ga[j], be[j]);
+                ln_st<T, V>(y + (long long)i * V, f[k].rounded());
             }
         }
         if (P.mean && lane == 0) {
@@ -188,12 +214,18 @@ __global__ void __launch_bounds__(L == 0 ? LN_BWD_MAX_BLOCK : LN_THREADS) layer_
     const int groups = L == 0 ? 1 : LN_THREADS / L, group = L == 0 ? 0 : (int)threadIdx.x / L;
     const float inv_c = 1.f / (float)P.c;
     const long long step = (long long)gridDim.x * groups;
-    float sg[SUMS ? VPL : 1][V], sb[SUMS ? VPL : 1][V];
+    constexpr int N = (V + 1) / 2;
+    float2 sg[SUMS ? VPL : 1][N], sb[SUMS ? VPL : 1][N], ga[VPL][N];
     if (SUMS)
 #pragma unroll
         for (int k = 0; k < VPL; ++k)
 #pragma unroll
-            for (int j = 0; j < V; ++j) sg[k][j] = sb[k][j] = 0.f;
+            for (int j = 0; j < N; ++j) sg[k][j] = sb[k][j] = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < VPL; ++k) {
+        const int i = lane + k * W;
+        ln_ldf<V>(P.gamma && i < P.nvec ? P.gamma + i * V : nullptr, ga[k], 1.f);
+    }
     LnVec<T, V> gn[VPL], xn[VPL];
     float mn = 0.f, rn = 0.f;
     auto fetch = [&](long long row) {
@@ -218,36 +250,32 @@ __global__ void __launch_bounds__(L == 0 ? LN_BWD_MAX_BLOCK : LN_THREADS) layer_
     long long row = (long long)blockIdx.x * groups + group;
     fetch(row);
     for (long long r0 = (long long)blockIdx.x * groups; r0 < P.rows; r0 += step, row += step) {
-        LnVec<T, V> gv[VPL], xv[VPL];
+        LnPairs<T, V> d[VPL], xh[VPL];  // g, from there g*gamma; x, from there xhat
 #pragma unroll
         for (int k = 0; k < VPL; ++k) {
-            gv[k] = gn[k];
-            xv[k] = xn[k];
+            d[k] = LnPairs<T, V>(gn[k]);
+            xh[k] = LnPairs<T, V>(xn[k]);
         }
         const float mean = mn, rstd = rn;
         if (r0 + step < P.rows) fetch(row + step);
-        float2 s = make_float2(0.f, 0.f);
+        float2 sa = make_float2(0.f, 0.f), sx = sa;
 #pragma unroll
-        for (int k = 0; k < VPL; ++k) {
-            const int i = lane + k * W;
-            if (i < P.nvec) {
-                float ga[V];
-                ln_ldf<V>(P.gamma ? P.gamma + i * V : nullptr, ga, 1.f);
+        for (int k = 0; k < VPL; ++k)
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float gj = to_f32<T>(gv[k].v[j]), xh = (to_f32<T>(xv[k].v[j]) - mean) * rstd, d = gj * ga[j];
-                    s.x += d;
-                    s.y = fmaf(d, xh, s.y);
-                    if (SUMS) {
-                        sg[k][j] = fmaf(gj, xh, sg[k][j]);
-                        sb[k][j] += gj;
-                    }
+            for (int j = 0; j < N; ++j) {  // (columns past the end have g = 0)
+                const float2 g = d[k].p[j], h = mul2(add2(xh[k].p[j], splat2(-mean)), splat2(rstd)), t = mul2(g, ga[k][j]);
+                sa = add2(sa, t);
+                sx = fma2(t, h, sx);
+                if (SUMS) {
+                    sg[k][j] = fma2(g, h, sg[k][j]);
+                    sb[k][j] = add2(sb[k][j], g);
                 }
+                d[k].p[j] = t;
+                xh[k].p[j] = h;
             }
-        }
-        s = ln_sum2<L>(s, red[turn]);
+        const float2 s = ln_sum2<L>(make_float2(sa.x + sa.y, sx.x + sx.y), red[turn]);
         turn ^= 1;
-        const float a = s.x * inv_c, b = s.y * inv_c;
+        const float2 r = splat2(rstd), a = splat2(-s.x * inv_c * rstd), b = splat2(-s.y * inv_c * rstd);
         if (row < P.rows) {
             T* dx = static_cast<T*>(P.dx) + row * P.ld_dx;
             const T* add = ADD ? static_cast<const T*>(P.add) + row * P.ld_add : nullptr;
@@ -255,18 +283,14 @@ __global__ void __launch_bounds__(L == 0 ? LN_BWD_MAX_BLOCK : LN_THREADS) layer_
             for (int k = 0; k < VPL; ++k) {
                 const int i = lane + k * W;
                 if (i < P.nvec) {
-                    float ga[V];
-                    ln_ldf<V>(P.gamma ? P.gamma + i * V : nullptr, ga, 1.f);
-                    LnVec<T, V> o, ad;
-                    if (ADD) ad = ln_ld<T, V>(add + (long long)i * V);
+                    LnPairs<T, V> ad;
+                    if (ADD) ad = LnPairs<T, V>(ln_ld<T, V>(add + (long long)i * V));
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const float xh = (to_f32<T>(xv[k].v[j]) - mean) * rstd, d = to_f32<T>(gv[k].v[j]) * ga[j];
-                        float v = rstd * (d - a - xh * b);
-                        if (ADD) v += to_f32<T>(ad.v[j]);
-                        o.v[j] = from_f32<T>(v);
+                    for (int j = 0; j < N; ++j) {
+                        d[k].p[j] = fma2(xh[k].p[j], b, fma2(d[k].p[j], r, a));
+                        if (ADD) d[k].p[j] = add2(d[k].p[j], ad.p[j]);
                     }
-                    ln_st<T, V>(dx + (long long)i * V, o);
+                    ln_st<T, V>(dx + (long long)i * V, d[k].rounded());
                 }
             }
         }
@@ -280,8 +304,8 @@ __global__ void __launch_bounds__(L == 0 ? LN_BWD_MAX_BLOCK : LN_THREADS) layer_
                 if (i < P.nvec)
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        out[i * V + j] = sg[k][j];
-                        out[P.c + i * V + j] = sb[k][j];
+                        out[i * V + j] = j & 1 ? sg[k][j / 2].y : sg[k][j / 2].x;
+                        out[P.c + i * V + j] = j & 1 ? sb[k][j / 2].y : sb[k][j / 2].x;
                     }
             }
         } else {
@@ -290,11 +314,13 @@ __global__ void __launch_bounds__(L == 0 ? LN_BWD_MAX_BLOCK : LN_THREADS) layer_
 #pragma unroll
             for (int k = 0; k < VPL; ++k)
 #pragma unroll
-                for (int j = 0; j < V; ++j)
+                for (int j = 0; j < N; ++j)
 #pragma unroll
                     for (int o = L; o < 32; o <<= 1) {
-                        sg[k][j] += __shfl_xor_sync(0xffffffffu, sg[k][j], o);
-                        sb[k][j] += __shfl_xor_sync(0xffffffffu, sb[k][j], o);
+                        sg[k][j].x += __shfl_xor_sync(0xffffffffu, sg[k][j].x, o);
+                        sg[k][j].y += __shfl_xor_sync(0xffffffffu, sg[k][j].y, o);
+                        sb[k][j].x += __shfl_xor_sync(0xffffffffu, sb[k][j].x, o);
+                        sb[k][j].y += __shfl_xor_sync(0xffffffffu, sb[k][j].y, o);
                     }
             for (int w = 0; w < LN_THREADS / 32; ++w) {
                 if ((int)(threadIdx.x >> 5) == w && (threadIdx.x & 31) < L) {
@@ -305,8 +331,8 @@ __global__ void __launch_bounds__(L == 0 ? LN_BWD_MAX_BLOCK : LN_THREADS) layer_
 #pragma unroll
                             for (int j = 0; j < V; ++j) {
                                 const int at = i * V + j;
-                                ln_cols[at] = (w ? ln_cols[at] : 0.f) + sg[k][j];
-                                ln_cols[P.c + at] = (w ? ln_cols[P.c + at] : 0.f) + sb[k][j];
+                                ln_cols[at] = (w ? ln_cols[at] : 0.f) + (j & 1 ? sg[k][j / 2].y : sg[k][j / 2].x);
+                                ln_cols[P.c + at] = (w ? ln_cols[P.c + at] : 0.f) + (j & 1 ? sb[k][j / 2].y : sb[k][j / 2].x);
                             }
                     }
                 }
@@ -364,26 +390,31 @@ template <typename T> __global__ void __launch_bounds__(128) layer_norm_cols_ker
     out[P.c + i] = sb;
 }
 
-// dgamma and dbeta from `parts` blocks' sums: 32 columns by 32 threads each, in fp64 and a fixed order.
-static __global__ void __launch_bounds__(1024) layer_norm_reduce_kernel(const float* __restrict__ partials, int parts, int c, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+// dgamma and dbeta from `parts` blocks' sums: 8 columns (a 32-byte sector) by 128 threads each, in fp64 and a fixed order.
+constexpr int LN_RED_COLS = 8, LN_RED_ROWS = 128;
+static __global__ void __launch_bounds__(LN_RED_COLS * LN_RED_ROWS) layer_norm_reduce_kernel(const float* __restrict__ partials, int parts, int c, float* __restrict__ dgamma, float* __restrict__ dbeta) {
     pdl_launch_dependents();
     pdl_wait();
-    __shared__ double red[32][33];
-    const int col = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
+    __shared__ double red[LN_RED_ROWS / 4][LN_RED_COLS];
+    const int j = threadIdx.x % LN_RED_COLS, w = threadIdx.x / LN_RED_COLS, col = blockIdx.x * LN_RED_COLS + j;
     double s = 0.0;
     if (col < 2 * c) {
         const float* p = partials + col;
         const size_t ld = 2 * (size_t)c;
 #pragma unroll 8
-        for (int b = w; b < parts; b += 32) s += (double)p[(size_t)b * ld];
+        for (int b = w; b < parts; b += LN_RED_ROWS) s += (double)p[(size_t)b * ld];
     }
-    red[w][threadIdx.x & 31] = s;
+    s += __shfl_xor_sync(0xffffffffu, s, 8);  // a warp holds four rows of the eight columns
+    s += __shfl_xor_sync(0xffffffffu, s, 16);
+    if ((threadIdx.x & 31) < LN_RED_COLS) red[w / 4][j] = s;
     __syncthreads();
-    s = red[threadIdx.x & 31][w];  // column w of the 32, summed by this warp
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    const int out = blockIdx.x * 32 + w;
-    if ((threadIdx.x & 31) == 0 && out < 2 * c) (out < c ? dgamma[out] : dbeta[out - c]) = (float)s;
+    if (threadIdx.x < 32) {  // four threads a column
+        s = 0.0;
+        for (int b = threadIdx.x / LN_RED_COLS; b < LN_RED_ROWS / 4; b += 4) s += red[b][j];
+        s += __shfl_xor_sync(0xffffffffu, s, 8);
+        s += __shfl_xor_sync(0xffffffffu, s, 16);
+        if (threadIdx.x < LN_RED_COLS && col < 2 * c) (col < c ? dgamma[col] : dbeta[col - c]) = (float)s;
+    }
 }
 
 }  // namespace nbcbs
