@@ -21,6 +21,8 @@ NB_DTYPE_F32, NB_DTYPE_BF16, NB_DTYPE_F16 = 0, 1, 2
 NB_MODE_BF16_TC, NB_MODE_F32_REF, NB_MODE_F16_TC = 0, 1, 2
 NB_CBS_FLAG_FORCE_SIMT = 1
 NB_CBS_FLAG_SEPARATE_FINALIZE = 2
+NB_ACT_NONE, NB_ACT_SILU, NB_ACT_GELU = 0, 1, 2
+NB_LINEAR_FLAG_FORCE_SIMT = 1
 
 EXPORTS = (
     "nb_abi_version", "nb_last_error", "nb_cbs_plan_create", "nb_cbs_plan_destroy", "nb_cbs_out_shape",
@@ -33,6 +35,8 @@ EXPORTS = (
     "nb_cbs_plan_set_dx_target", "nb_cbs_plan_set_fwd_residual", "nb_cbs_plan_set_bwd_residual",
     "nb_adamw_plan_create", "nb_adamw_plan_destroy", "nb_adamw_workspace_bytes", "nb_adamw_upload", "nb_adamw_step", "nb_adamw_step_scaled",
     "nb_layer_norm_fwd", "nb_layer_norm_workspace_bytes", "nb_layer_norm_bwd",
+    "nb_linear_plan_create", "nb_linear_plan_destroy", "nb_linear_workspace_bytes", "nb_linear_paths", "nb_linear_poll_status", "nb_linear_fwd",
+    "nb_linear_bwd_data", "nb_linear_bwd_weight", "nb_act_bwd",
 )
 
 
@@ -66,6 +70,10 @@ class nb_adamw_tensor(Structure):
 class nb_adamw_hyper(Structure):
     _fields_ = [("struct_size", c_uint32), ("eps", c_float), ("max_norm", c_float), ("lr", c_float * 3), ("weight_decay", c_float * 3),
                 ("beta1", c_double), ("beta2", c_double)]
+
+
+class nb_linear_desc(Structure):
+    _fields_ = [("struct_size", c_uint32), ("c_in", c_int32), ("c_out", c_int32), ("dtype", c_int32), ("flags", c_uint32)]
 
 
 class NbError(RuntimeError):
@@ -128,6 +136,15 @@ def load() -> ctypes.CDLL:
         lib.nb_layer_norm_fwd.argtypes = [c_int32, c_int64, c_int32, V, c_int64, FP, FP, c_float, V, c_int64, FP, FP, V]
         lib.nb_layer_norm_workspace_bytes.argtypes = [c_int64, c_int32, POINTER(c_size_t)]
         lib.nb_layer_norm_bwd.argtypes = [c_int32, c_int64, c_int32, V, c_int64, V, c_int64, FP, FP, FP, V, c_int64, V, c_int64, FP, FP, V, c_size_t, V]
+        lib.nb_linear_plan_create.argtypes = [POINTER(nb_linear_desc), c_int, POINTER(V)]
+        lib.nb_linear_plan_destroy.argtypes = [V]
+        lib.nb_linear_workspace_bytes.argtypes = [V, c_int64, POINTER(c_size_t)]
+        lib.nb_linear_paths.argtypes = [V, c_int64, POINTER(c_int32)]
+        lib.nb_linear_poll_status.argtypes = [V, V]
+        lib.nb_linear_fwd.argtypes = [V, c_int64, V, c_int64, V, FP, c_int32, V, c_int64, V, V, c_int64, V, c_size_t, V]
+        lib.nb_linear_bwd_data.argtypes = [V, c_int64, V, c_int64, V, V, c_int32, V, c_int64, V, c_int64, V, c_size_t, V]
+        lib.nb_linear_bwd_weight.argtypes = [V, c_int64, V, c_int64, V, c_int64, FP, FP, V, c_size_t, V]
+        lib.nb_act_bwd.argtypes = [c_int32, c_int64, c_int32, V, V, V, V]
         lib.nb_slice_add.argtypes = [c_int32, ctypes.c_int64, c_int32, V, ctypes.c_int64, V, ctypes.c_int64, V, ctypes.c_int64, c_int32, V]
         lib.nb_maxpool5_fwd.argtypes = [c_int32, c_int32, c_int32, c_int32, c_int32, V, V, V, ctypes.c_int64, ctypes.c_int64, V]
         lib.nb_maxpool5_bwd.argtypes = [c_int32, c_int32, c_int32, c_int32, c_int32, V, V, V, c_int32, ctypes.c_int64, ctypes.c_int64, V]
@@ -543,3 +560,60 @@ class AdamWPlan:
             self.close()
         except Exception:
             pass
+
+
+class LinearPlan:
+    """Owner of one nb_linear_plan handle: a layer of c_in -> c_out channels, any number of rows."""
+
+    def __init__(self, c_in, c_out, dtype, device=0, flags=0):
+        self.c_in, self.c_out, self.dtype, self.device = int(c_in), int(c_out), int(dtype), device
+        self.handle = c_void_p()
+        desc = nb_linear_desc(ctypes.sizeof(nb_linear_desc), self.c_in, self.c_out, self.dtype, flags)
+        _check(load().nb_linear_plan_create(byref(desc), device, byref(self.handle)))
+
+    def workspace_bytes(self, rows) -> int:
+        b = c_size_t()
+        _check(load().nb_linear_workspace_bytes(self.handle, int(rows), byref(b)))
+        return b.value
+
+    def paths(self, rows):
+        p3 = (c_int32 * 3)()
+        _check(load().nb_linear_paths(self.handle, int(rows), p3))
+        return {"fwd": p3[0], "data": p3[1], "weight": p3[2]}
+
+    def poll(self, stream=None):
+        _check(load().nb_linear_poll_status(self.handle, _stream_on(stream, self.device)))
+
+    def close(self):
+        if self.handle:
+            load().nb_linear_plan_destroy(self.handle)
+            self.handle = c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def nb_linear_fwd(plan: LinearPlan, rows, x, w, bias, act, out, workspace, z=None, res=None, ld_x=0, ld_out=0, ld_res=0, stream=None):
+    """out = act(x w^T + bias) + res; z, where given, receives x w^T + bias."""
+    _check(load().nb_linear_fwd(plan.handle, int(rows), _ptr(x), int(ld_x), _ptr(w), _ptr(bias), int(act), _ptr(res), int(ld_res), _ptr(z), _ptr(out), int(ld_out),
+                                _ptr(workspace), _nbytes(workspace), _stream_on(stream, plan.device)))
+
+
+def nb_linear_bwd_data(plan: LinearPlan, rows, dy, w, dx, workspace, z_in=None, act_in=NB_ACT_NONE, add=None, ld_dy=0, ld_dx=0, ld_add=0, stream=None):
+    """dx = (dy w + add) * act_in'(z_in)."""
+    _check(load().nb_linear_bwd_data(plan.handle, int(rows), _ptr(dy), int(ld_dy), _ptr(w), _ptr(z_in), int(act_in), _ptr(add), int(ld_add), _ptr(dx), int(ld_dx),
+                                     _ptr(workspace), _nbytes(workspace), _stream_on(stream, plan.device)))
+
+
+def nb_linear_bwd_weight(plan: LinearPlan, rows, x, dy, dw, dbias, workspace, ld_x=0, ld_dy=0, stream=None):
+    """dw = dy^T x and, where dbias is given, the sums of dy over the rows."""
+    _check(load().nb_linear_bwd_weight(plan.handle, int(rows), _ptr(x), int(ld_x), _ptr(dy), int(ld_dy), _ptr(dw), _ptr(dbias), _ptr(workspace), _nbytes(workspace),
+                                       _stream_on(stream, plan.device)))
+
+
+def nb_act_bwd(dtype, n, act, dy, z, dz, stream=None):
+    """dz = dy * act'(z) over n elements."""
+    _check(load().nb_act_bwd(int(dtype), int(n), int(act), _ptr(dy), _ptr(z), _ptr(dz), _stream(stream)))

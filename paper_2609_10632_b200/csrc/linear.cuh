@@ -1,0 +1,366 @@
+// Matrix products of MLP layers on the CUDA cores, their activations, and the sums of split products (see include/nb_linear.h
+// for the arithmetic; the tensor-core kernel is tc_linear.cuh).
+#pragma once
+#include "../../include/nb_linear.h"
+#include "common.cuh"
+
+namespace nbcbs {
+
+enum { LIN_FWD = 0, LIN_DATA = 1, LIN_WEIGHT = 2 };
+
+// ------------------------------------------------------------------------------------------ activations, fp32
+__device__ __forceinline__ float lin_act(float z, int act) {
+    if (act == NB_ACT_SILU) return z / (1.f + expf(-z));
+    if (act == NB_ACT_GELU) return 0.5f * z * erfcf(-0.70710678f * z);
+    return z;
+}
+__device__ __forceinline__ float lin_act_grad(float z, int act) {
+    if (act == NB_ACT_SILU) {
+        const float s = 1.f / (1.f + expf(-z));
+        return s * (1.f + z * (1.f - s));
+    }
+    if (act == NB_ACT_GELU) return fmaf(z * 0.39894228f, expf(-0.5f * z * z), 0.5f * erfcf(-0.70710678f * z));
+    return 1.f;
+}
+
+// ------------------------------------------------------------------------------------------ the same for 16-bit results
+// Phi(z) - 1/2 of two values: an odd polynomial of degree 17 on [-4.2, 4.2], fitted here (least squares with Lawson's weights, its
+// end held at 1/2 so that it is exact beyond), |error| <= 1.8e-5 in fp32.  No special-function unit: that one is half
+// as fast as the epilogue of a product with few terms needs.
+__device__ __forceinline__ float2 lin_phi2(float2 z) {
+    z.x = fminf(fmaxf(z.x, -4.2f), 4.2f);
+    z.y = fminf(fmaxf(z.y, -4.2f), 4.2f);
+    const float2 u = mul2(z, z);
+    float2 p = fma2(u, splat2(6.210412045737357e-11f), splat2(-5.7821978316496825e-09f));
+    p = fma2(p, u, splat2(2.386405242305045e-07f));
+    p = fma2(p, u, splat2(-5.825401785841677e-06f));
+    p = fma2(p, u, splat2(9.512664109934121e-05f));
+    p = fma2(p, u, splat2(-0.0011167984921485186f));
+    p = fma2(p, u, splat2(0.009836794808506966f));
+    p = fma2(p, u, splat2(-0.06636778265237808f));
+    p = fma2(p, u, splat2(0.3989098072052002f));
+    p = mul2(p, z);
+    return make_float2(fminf(fmaxf(p.x, -0.5f), 0.5f), fminf(fmaxf(p.y, -0.5f), 0.5f));
+}
+__device__ __forceinline__ float2 lin_tanh2(float2 h) {
+    float2 t;
+    asm("tanh.approx.f32 %0, %1;" : "=f"(t.x) : "f"(h.x));
+    asm("tanh.approx.f32 %0, %1;" : "=f"(t.y) : "f"(h.y));
+    return t;
+}
+__device__ __forceinline__ float2 lin_act2(float2 z, int act) {
+    if (act == NB_ACT_GELU) return fma2(z, lin_phi2(z), mul2(z, splat2(0.5f)));
+    if (act == NB_ACT_SILU) {
+        const float2 h = mul2(z, splat2(0.5f));
+        return fma2(h, lin_tanh2(h), h);
+    }
+    return z;
+}
+__device__ __forceinline__ float2 lin_act_grad2(float2 z, int act) {
+    if (act == NB_ACT_GELU) {
+        const float2 e = mul2(mul2(z, z), splat2(-0.72134752f));  // -z^2/2 in base 2
+        float2 d;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d.x) : "f"(e.x));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d.y) : "f"(e.y));
+        // (an infinite z would make inf * 0 of the second term: a z beyond 64 counts as 64, where that term is zero)
+        const float2 c = make_float2(fminf(fmaxf(z.x, -64.f), 64.f), fminf(fmaxf(z.y, -64.f), 64.f));
+        return fma2(mul2(c, splat2(0.39894228f)), d, add2(lin_phi2(z), splat2(0.5f)));
+    }
+    if (act == NB_ACT_SILU) {
+        const float2 s = fma2(lin_tanh2(mul2(z, splat2(0.5f))), splat2(0.5f), splat2(0.5f));
+        const float2 q = fma2(s, splat2(-1.f), splat2(1.f));
+        return mul2(s, fma2(z, q, splat2(1.f)));
+    }
+    return splat2(1.f);
+}
+
+// ------------------------------------------------------------------------------------------ products on plain FMA units
+// C[m][n] = sum_k A(m,k) B(n,k):
+//   LIN_FWD     m = row,   n = c_out, k = c_in   A = x [m][k], B = w [n][k]
+//   LIN_DATA    m = row,   n = c_in,  k = c_out  A = dy [m][k], B = w [k][n]
+//   LIN_WEIGHT  m = c_out, n = c_in,  k = row    A = dy [k][m], B = x [k][n]
+struct LinArgs {
+    const void *a, *b;
+    long long lda, ldb;
+    long long M, N, K, kslice;  // kslice: products of a slice (blockIdx.z), a multiple of LS_BK
+    int slices;
+    float* partial;  // slices > 1: [slices][M][N]
+    // epilogue
+    const float* bias;
+    int act;
+    const void *add, *zin;  // residual / other branch's gradient [M][N] with pitch ld_add; z_in [M][N]
+    long long ld_add;
+    void* z;                // [M][N]
+    void* out;              // LIN_WEIGHT: fp32
+    long long ld_out;
+};
+
+template <typename T, int KIND> __device__ __forceinline__ void lin_store(const LinArgs& P, long long m, long long n, float v) {
+    if (KIND == LIN_WEIGHT) {
+        static_cast<float*>(P.out)[m * P.ld_out + n] = v;
+        return;
+    }
+    if (KIND == LIN_FWD) {
+        if (P.bias) v += P.bias[n];
+        if (P.z) static_cast<T*>(P.z)[m * P.N + n] = from_f32<T>(v);
+        v = lin_act(v, P.act);
+        if (P.add) v += to_f32<T>(static_cast<const T*>(P.add)[m * P.ld_add + n]);
+    } else {
+        if (P.add) v += to_f32<T>(static_cast<const T*>(P.add)[m * P.ld_add + n]);
+        if (P.zin) v *= lin_act_grad(to_f32<T>(static_cast<const T*>(P.zin)[m * P.N + n]), P.act);
+    }
+    static_cast<T*>(P.out)[m * P.ld_out + n] = from_f32<T>(v);
+}
+
+// Bound: FMA issue.  A block of 256 threads has a [64 x 64] tile, a thread [4 x 4] of it; operand tiles of 16 k travel through
+// registers into shared memory as fp32, k-major, double-buffered.  VEC: every operand row is whole vectors of four.
+constexpr int LS_BM = 64, LS_BN = 64, LS_BK = 16, LS_THREADS = 256, LS_PITCH = 68;
+
+// Four elements of an operand stored [outer][inner] at (outer, inner..inner+3) as fp32, zeros outside.
+template <typename T, bool VEC> __device__ __forceinline__ float4 ls_load(const T* p, long long ld, long long outer, long long inner, long long outers, long long inners) {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (outer >= outers) return v;
+    const T* q = p + outer * ld + inner;
+    if (VEC) {
+        if (inner < inners) {
+            if constexpr (sizeof(T) == 4) {
+                v = *reinterpret_cast<const float4*>(q);
+            } else {
+                const uint2 r = *reinterpret_cast<const uint2*>(q);
+                const float2 lo = pair_to_f32<T>(reinterpret_cast<const T*>(&r.x)), hi = pair_to_f32<T>(reinterpret_cast<const T*>(&r.y));
+                v = make_float4(lo.x, lo.y, hi.x, hi.y);
+            }
+        }
+    } else {
+        if (inner < inners) v.x = to_f32<T>(q[0]);
+        if (inner + 1 < inners) v.y = to_f32<T>(q[1]);
+        if (inner + 2 < inners) v.z = to_f32<T>(q[2]);
+        if (inner + 3 < inners) v.w = to_f32<T>(q[3]);
+    }
+    return v;
+}
+
+template <typename T, int KIND, bool VEC> __global__ void __launch_bounds__(LS_THREADS) lin_simt_kernel(LinArgs P) {
+    pdl_launch_dependents();
+    pdl_wait();
+    __shared__ __align__(16) float sA[2][LS_BK][LS_PITCH], sB[2][LS_BK][LS_PITCH];
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    const long long tiles_n = (P.N + LS_BN - 1) / LS_BN;
+    const long long m0 = blockIdx.x / tiles_n * LS_BM, n0 = blockIdx.x % tiles_n * LS_BN;
+    const long long k0 = (long long)blockIdx.z * P.kslice, k1 = k0 + P.kslice < P.K ? k0 + P.kslice : P.K;
+    const T* A = static_cast<const T*>(P.a);
+    const T* B = static_cast<const T*>(P.b);
+    constexpr bool A_K = KIND != LIN_WEIGHT, B_K = KIND == LIN_FWD;  // k is the contiguous index of the operand
+    // [outer][k]: 64 outer x 4 groups of four k; [k][outer]: 16 k x 16 groups of four outer
+    const int ro = tid & 63, rk = (tid >> 6) * 4, co = (tid & 15) * 4, ck = tid >> 4;
+    float4 ra, rb;
+    auto fetch = [&](long long k) {
+        ra = A_K ? ls_load<T, VEC>(A, P.lda, m0 + ro, k + rk, P.M, k1) : ls_load<T, VEC>(A, P.lda, k + ck, m0 + co, k1, P.M);
+        rb = B_K ? ls_load<T, VEC>(B, P.ldb, n0 + ro, k + rk, P.N, k1) : ls_load<T, VEC>(B, P.ldb, k + ck, n0 + co, k1, P.N);
+    };
+    auto put = [&](int s) {
+        if (A_K) {
+            sA[s][rk][ro] = ra.x; sA[s][rk + 1][ro] = ra.y; sA[s][rk + 2][ro] = ra.z; sA[s][rk + 3][ro] = ra.w;
+        } else {
+            *reinterpret_cast<float4*>(&sA[s][ck][co]) = ra;
+        }
+        if (B_K) {
+            sB[s][rk][ro] = rb.x; sB[s][rk + 1][ro] = rb.y; sB[s][rk + 2][ro] = rb.z; sB[s][rk + 3][ro] = rb.w;
+        } else {
+            *reinterpret_cast<float4*>(&sB[s][ck][co]) = rb;
+        }
+    };
+    float2 acc[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = make_float2(0.f, 0.f);
+    fetch(k0);
+    put(0);
+    __syncthreads();
+    int s = 0;
+    for (long long k = k0; k < k1; k += LS_BK) {
+        const bool more = k + LS_BK < k1;
+        if (more) fetch(k + LS_BK);
+#pragma unroll
+        for (int kk = 0; kk < LS_BK; ++kk) {
+            const float4 a = *reinterpret_cast<const float4*>(&sA[s][kk][ty * 4]), b = *reinterpret_cast<const float4*>(&sB[s][kk][tx * 4]);
+            const float2 b0 = make_float2(b.x, b.y), b1 = make_float2(b.z, b.w);
+            const float av[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                acc[i][0] = fma2(splat2(av[i]), b0, acc[i][0]);
+                acc[i][1] = fma2(splat2(av[i]), b1, acc[i][1]);
+            }
+        }
+        if (more) {
+            s ^= 1;
+            put(s);  // (the other buffer: its readers passed the barrier of the round before)
+            __syncthreads();
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const long long m = m0 + ty * 4 + i;
+        if (m >= P.M) break;
+        const float v[4] = {acc[i][0].x, acc[i][0].y, acc[i][1].x, acc[i][1].y};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const long long n = n0 + tx * 4 + j;
+            if (n >= P.N) break;
+            if (P.slices > 1) P.partial[((long long)blockIdx.z * P.M + m) * P.N + n] = v[j];
+            else lin_store<T, KIND>(P, m, n, v[j]);
+        }
+    }
+}
+
+// Adds the slices of a product (fp64, in their order) and finishes it.
+template <typename T, int KIND> __global__ void __launch_bounds__(256) lin_slices_kernel(LinArgs P) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const long long n = P.M * P.N;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        double s = 0.0;
+        for (int z = 0; z < P.slices; ++z) s += (double)P.partial[z * n + i];
+        lin_store<T, KIND>(P, i / P.N, i % P.N, (float)s);
+    }
+}
+
+// Partial sums of dy over ranges of rows: [gridDim.y][c], 32 columns a block.
+template <typename T> __global__ void __launch_bounds__(256) lin_colsum_kernel(const T* __restrict__ dy, long long ld, long long rows, int c, long long per, float* __restrict__ partial) {
+    pdl_launch_dependents();
+    pdl_wait();
+    __shared__ float red[8][33];
+    const int col = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
+    const long long r0 = (long long)blockIdx.y * per, r1 = r0 + per < rows ? r0 + per : rows;
+    float s = 0.f;
+    if (col < c)
+#pragma unroll 4
+        for (long long r = r0 + w; r < r1; r += 8) s += to_f32<T>(dy[r * ld + col]);
+    red[w][threadIdx.x & 31] = s;
+    __syncthreads();
+    if (w == 0 && col < c) {
+        double t = 0.0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t += (double)red[k][threadIdx.x & 31];
+        partial[(size_t)blockIdx.y * c + col] = (float)t;
+    }
+}
+// dw (n1 elements, `s1` slices) and dbias (n2 elements, `s2` slices) from their slices, in one launch; a count of zero slices: nothing to add.
+static __global__ void __launch_bounds__(256) lin_weight_sums_kernel(const float* __restrict__ p1, int s1, long long n1, float* __restrict__ o1, const float* __restrict__ p2, int s2, int n2,
+                                                                     float* __restrict__ o2) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const long long at = (long long)blockIdx.x * 256 + threadIdx.x, step = (long long)gridDim.x * 256;
+    if (s1 && (n1 & 3) == 0) {
+        for (long long v = at; v < n1 / 4; v += step) {
+            double s[4] = {0.0, 0.0, 0.0, 0.0};
+            for (int z0 = 0; z0 < s1; z0 += 8) {  // eight slices in flight
+                float4 a[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (z0 + u < s1) a[u] = reinterpret_cast<const float4*>(p1 + (long long)(z0 + u) * n1)[v];
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (z0 + u < s1) {
+                        s[0] += (double)a[u].x;
+                        s[1] += (double)a[u].y;
+                        s[2] += (double)a[u].z;
+                        s[3] += (double)a[u].w;
+                    }
+            }
+            reinterpret_cast<float4*>(o1)[v] = make_float4((float)s[0], (float)s[1], (float)s[2], (float)s[3]);
+        }
+    } else if (s1) {
+        for (long long i = at; i < n1; i += step) {
+            double s = 0.0;
+            for (int z = 0; z < s1; ++z) s += (double)p1[z * n1 + i];
+            o1[i] = (float)s;
+        }
+    }
+    if (s2)
+        for (long long i = at; i < n2; i += step) {
+            double s = 0.0;
+            for (int z = 0; z < s2; ++z) s += (double)p2[(long long)z * n2 + i];
+            o2[i] = (float)s;
+        }
+}
+
+// ------------------------------------------------------------------------------------------ a few rows: the weights are streamed once
+// Forward product of R rows (1, 2, 4 or 8): bound by the bytes of w.  WPC warps share a column of the output (a row of w); a
+// lane takes 16-byte pieces of it, several in flight, against the same pieces of every row of x, which L1 holds.
+constexpr int LR_THREADS = 256;
+template <typename T, int R> __global__ void __launch_bounds__(LR_THREADS) lin_rows_kernel(LinArgs P, int rows, int wpc) {
+    pdl_launch_dependents();
+    pdl_wait();
+    constexpr int V = 16 / (int)sizeof(T);
+    __shared__ float red[LR_THREADS / 32][R];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int cols = LR_THREADS / 32 / wpc, part = warp % wpc;
+    const long long n = (long long)blockIdx.x * cols + warp / wpc;
+    const bool live = n < P.N;
+    const int nvec = (int)(P.K / V);
+    const T* x = static_cast<const T*>(P.a);
+    const T* w = static_cast<const T*>(P.b) + (live ? n : 0) * P.ldb;
+    float2 acc[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) acc[r] = make_float2(0.f, 0.f);
+    constexpr int U = 4;
+    const int stride = 32 * wpc;
+    for (int i0 = part * 32 + lane; i0 < nvec; i0 += U * stride) {
+        Vec16<T> wv[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (live && i0 + u * stride < nvec) wv[u] = ld16_stream(w + (long long)(i0 + u * stride) * V);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * stride;
+            if (!live || i >= nvec) break;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (r >= rows) break;
+                const Vec16<T> xv = ld16(x + (long long)r * P.lda + (long long)i * V);
+#pragma unroll
+                for (int j = 0; j < V; j += 2) acc[r] = fma2(pair_to_f32<T>(xv.v + j), pair_to_f32<T>(wv[u].v + j), acc[r]);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        float s = acc[r].x + acc[r].y;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (lane == 0) red[warp][r] = s;
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < cols * rows; e += LR_THREADS) {
+        const int c = e % cols, r = e / cols;
+        const long long nn = (long long)blockIdx.x * cols + c;
+        float s = 0.f;
+        for (int p = 0; p < wpc; ++p) s += red[c * wpc + p][r];
+        if (nn < P.N) lin_store<T, LIN_FWD>(P, r, nn, s);
+    }
+}
+
+// ------------------------------------------------------------------------------------------ dz = dy * act'(z)
+template <typename T, bool VEC> __global__ void __launch_bounds__(256) lin_act_bwd_kernel(const T* dy, const T* z, T* dz, long long n, int act) {
+    pdl_launch_dependents();
+    pdl_wait();
+    constexpr int V = VEC ? 16 / (int)sizeof(T) : 1;
+    const long long nv = n / V, step = (long long)gridDim.x * 256;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < nv; i += step) {
+        if constexpr (VEC) {
+            const Vec16<T> g = ld16_stream(dy + i * V), x = ld16_stream(z + i * V);
+            Vec16<T> o;
+#pragma unroll
+            for (int j = 0; j < V; ++j) o.v[j] = from_f32<T>(to_f32<T>(g.v[j]) * lin_act_grad(to_f32<T>(x.v[j]), act));
+            st16(dz + i * V, o);
+        } else {
+            dz[i] = from_f32<T>(to_f32<T>(dy[i]) * lin_act_grad(to_f32<T>(z[i]), act));
+        }
+    }
+    if (VEC && blockIdx.x == 0 && threadIdx.x < n - nv * V) {
+        const long long i = nv * V + threadIdx.x;
+        dz[i] = from_f32<T>(to_f32<T>(dy[i]) * lin_act_grad(to_f32<T>(z[i]), act));
+    }
+}
+
+}  // namespace nbcbs

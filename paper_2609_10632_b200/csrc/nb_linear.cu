@@ -1,0 +1,494 @@
+// C ABI of the MLP products (see include/nb_linear.h): plans, the choice of kernels and tiles, the three calls.  The only
+// allocation is a plan's status block; the workspace is the caller's.
+#include <algorithm>
+#include <atomic>
+#include <cstring>
+#include <memory>
+#include <new>
+
+#include "api_common.cuh"
+#include "linear.cuh"
+#include "tc_common.cuh"
+#include "tc_linear.cuh"
+
+using namespace nbcbs;
+using namespace nbapi;
+
+struct nb_linear_plan_s {
+    nb_linear_desc d;
+    int device = 0, sms = 148;
+    int* status = nullptr;
+};
+
+namespace {
+
+size_t size_of(int32_t dtype) { return dtype == NB_DTYPE_F32 ? 4 : 2; }
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+// ---------------------------------------------------------------- tensor cores: tiles
+struct TlCfg {
+    bool cg2 = false;
+    int bn = 0, m_tiles = 0, n_tiles = 0, kblocks = 0, splits = 1, kb_per_split = 0;
+    double cost = 0;
+};
+
+// Cycles of a stage (128 rows a CTA, BN columns, 64 k): the products, or the operand bytes from L2 at what an SM gets of them.
+double stage_cycles(bool cg2, int bn) {
+    const double bytes = 16384.0 + (cg2 ? bn / 2 : bn) * 128.0;
+    return std::max(2.0 * bn, bytes / 55.0);
+}
+
+// Tiles of a forward product or data gradient: the least time of the persistent loop over what the candidates give.
+TlCfg choose_rows(long long M, long long N, long long K, int sms, double epi_instr) {
+    TlCfg best;
+    for (int cg2 = 1; cg2 >= 0; --cg2)
+        for (int bn = 256; bn >= 64; bn -= 64) {
+            TlCfg c;
+            c.cg2 = cg2 != 0;
+            c.bn = bn;
+            c.m_tiles = (int)ceil_div(M, cg2 ? 256 : 128);
+            c.n_tiles = (int)ceil_div(N, bn);
+            c.kblocks = (int)ceil_div(K, TL_KC);
+            const long long workers = cg2 ? sms / 2 : sms, tiles = (long long)c.m_tiles * c.n_tiles;
+            const double main = c.kblocks * stage_cycles(cg2, bn), epi = bn * epi_instr;
+            c.cost = (double)ceil_div(tiles, workers) * std::max(main, epi) + std::min(main, epi) + 1000.0;
+            if (!best.bn || c.cost < best.cost) best = c;
+        }
+    return best;
+}
+
+// Tiles and row slices of a weight gradient: every item is a CTA (or pair) of its own.
+TlCfg choose_weight(long long M, long long N, long long K, int sms) {
+    TlCfg best;
+    for (int cg2 = 1; cg2 >= 0; --cg2)
+        for (int bn = 256; bn >= 64; bn -= 64) {
+            TlCfg c;
+            c.cg2 = cg2 != 0;
+            c.bn = bn;
+            c.m_tiles = (int)ceil_div(M, cg2 ? 256 : 128);
+            c.n_tiles = (int)ceil_div(N, bn);
+            c.kblocks = (int)ceil_div(K, TL_KC);
+            const long long workers = cg2 ? sms / 2 : sms, tiles = (long long)c.m_tiles * c.n_tiles;
+            const long long most = std::max<long long>(1, std::min<long long>({64, c.kblocks, ceil_div(4 * workers, tiles)}));
+            for (long long s = 1; s <= most; ++s) {
+                c.kb_per_split = (int)ceil_div(c.kblocks, s);
+                c.splits = (int)ceil_div(c.kblocks, c.kb_per_split);
+                const double item = c.kb_per_split * stage_cycles(cg2, bn) + bn * 8.0 + 1500.0;
+                // (slices: written, read back and added at about 2.5 KB a cycle, and another launch)
+                const double sums = c.splits > 1 ? 3000.0 + 2.0 * c.splits * (double)M * N * 4 / 2500.0 : 0.0;
+                c.cost = (double)ceil_div(tiles * c.splits, workers) * item + sums;
+                if (!best.bn || c.cost < best.cost) best = c;
+            }
+        }
+    return best;
+}
+
+// ---------------------------------------------------------------- CUDA cores: slices of k
+struct SimtCfg {
+    long long tiles = 0, kslice = 0;
+    int slices = 1;
+};
+SimtCfg simt_cfg(long long M, long long N, long long K, int sms, bool weight) {
+    SimtCfg c;
+    c.tiles = ceil_div(M, LS_BM) * ceil_div(N, LS_BN);
+    // as many slices as fill the GPU, of 128 products or more each; sums over rows also in slices of at most 4096, which bounds the
+    // rounding errors of an fp32 sum
+    long long s = c.tiles >= sms ? 1 : std::min<long long>(ceil_div(2 * sms, c.tiles), std::max<long long>(1, K / 128));
+    if (weight) s = std::max(s, ceil_div(K, 4096));
+    s = std::min<long long>(s, 1024);
+    c.kslice = ceil_div(ceil_div(K, s), LS_BK) * LS_BK;
+    c.slices = (int)ceil_div(K, c.kslice);
+    return c;
+}
+int colsum_parts(long long rows) { return (int)std::max<long long>(1, std::min<long long>(64, rows / 256)); }
+
+// ---------------------------------------------------------------- choice of kernels
+bool tc_layer(const nb_linear_plan_s* p) {
+    return p->d.dtype != NB_DTYPE_F32 && !(p->d.flags & NB_LINEAR_FLAG_FORCE_SIMT) && p->d.c_in % 8 == 0 && p->d.c_out % 8 == 0;
+}
+bool few_rows(const nb_linear_plan_s* p, long long rows) { return rows <= 8 && ((size_t)p->d.c_in * size_of(p->d.dtype)) % 16 == 0; }
+bool whole16(const void* q, long long ld, size_t es) { return !(reinterpret_cast<uintptr_t>(q) & 15u) && ((size_t)ld * es) % 16 == 0; }
+
+size_t simt_ws(const nb_linear_plan_s* p, long long rows, int kind) {
+    const long long ci = p->d.c_in, co = p->d.c_out;
+    const long long M = kind == LIN_WEIGHT ? co : rows, N = kind == LIN_FWD ? co : ci, K = kind == LIN_FWD ? ci : kind == LIN_DATA ? co : rows;
+    const SimtCfg c = simt_cfg(M, N, K, p->sms, kind == LIN_WEIGHT);
+    size_t b = c.slices > 1 ? align_up((size_t)c.slices * M * N * 4, 256) : 0;
+    if (kind == LIN_WEIGHT) b += align_up((size_t)colsum_parts(rows) * co * 4, 256);
+    return b;
+}
+size_t tc_weight_ws(const nb_linear_plan_s* p, const TlCfg& c) {
+    const size_t M = p->d.c_out, N = p->d.c_in;
+    return (c.splits > 1 ? align_up((size_t)c.splits * M * N * 4, 256) : 0) + align_up((size_t)c.splits * c.n_tiles * M * 4, 256);
+}
+size_t workspace_for(const nb_linear_plan_s* p, long long rows) {
+    size_t b = 256;
+    for (int kind = 0; kind < 3; ++kind) b = std::max(b, simt_ws(p, rows, kind));
+    if (tc_layer(p)) b = std::max(b, tc_weight_ws(p, choose_weight(p->d.c_out, p->d.c_in, rows, p->sms)));
+    return b;
+}
+
+// ---------------------------------------------------------------- tensor cores: launch
+bool encode(CUtensorMap* m, int32_t dtype, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box, CUtensorMapSwizzle sw, bool load) {
+    tcdetail::DriverFns& d = tcdetail::driver();
+    if (!d.tiled) return false;
+    const CUtensorMapDataType t = dtype == NB_DTYPE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == NB_DTYPE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    const cuuint32_t one[3] = {1, 1, 1};
+    return d.tiled(m, t, (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, sw,
+                   load ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// a matrix [rows][cols] of 16-bit elements, boxes of box_cols by box_rows
+bool encode2(CUtensorMap* m, int32_t dtype, const void* base, long long rows, long long cols, long long ld, int box_cols, int box_rows, bool load) {
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
+    return encode(m, dtype, base, 2, dims, strides, box, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, load);
+}
+
+template <typename T, int KIND, bool CG2, int NP> nb_status launch_tc(const nb_linear_plan_s* plan, const TcLinParams& P, unsigned grid, size_t smem, cudaStream_t st) {
+    static std::atomic<unsigned long long> attr_set{0};  // one bit per device ordinal
+    const unsigned long long bit = 1ull << (plan->device & 63);
+    if (!(attr_set.load(std::memory_order_acquire) & bit)) {
+        NB_CUDA_CHECK(cudaFuncSetAttribute(tc_linear_kernel<T, KIND, CG2, NP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tcdetail::kMaxSmem));
+        attr_set.fetch_or(bit, std::memory_order_release);
+    }
+    launch_k(tc_linear_kernel<T, KIND, CG2, NP>, dim3(grid), dim3(TL_THREADS), smem, st, CG2 ? 2 : 1, P);
+    return launch_ok("tc_linear");
+}
+
+template <int KIND> nb_status run_tc(const nb_linear_plan_s* plan, const TlCfg& c, TcLinParams& P, cudaStream_t st) {
+    const bool f16 = plan->d.dtype == NB_DTYPE_F16;
+    P.kblocks = c.kblocks;
+    P.BN = c.bn;
+    P.m_tiles = c.m_tiles;
+    P.n_tiles = c.n_tiles;
+    P.group_m = 8;
+    P.acc_stride = 256;
+    P.splits = c.splits;
+    P.kb_per_split = c.kb_per_split;
+    P.status = plan->status;
+    const int own = c.cg2 ? c.bn / 2 : c.bn;
+    P.nblkB = (own + 63) / 64;
+    P.b_bytes = KIND == LIN_FWD ? (uint32_t)own * 128u : (uint32_t)P.nblkB * TL_BLK;
+    const int tm = c.cg2 ? 256 : 128;
+    P.idesc = ptx::make_idesc_bf16(tm, c.bn, KIND == LIN_WEIGHT, KIND != LIN_FWD, f16);
+    P.idesc_ones = ptx::make_idesc_bf16(tm, c.cg2 ? 32 : 16, 1, 1, f16);
+    P.bufs = KIND == LIN_WEIGHT ? 1 : 2;
+    const size_t fixed = 1024 + (size_t)8 * P.bufs * TL_STG + (KIND == LIN_WEIGHT ? TL_ONES_BYTES : 0) + 256;
+    P.stages = (int)std::min<size_t>(8, (tcdetail::kMaxSmem - fixed) / (TL_A_BYTES + P.b_bytes));
+    const size_t smem = fixed + (size_t)P.stages * (TL_A_BYTES + P.b_bytes);
+    const long long tiles = (long long)c.m_tiles * c.n_tiles * (KIND == LIN_WEIGHT ? c.splits : 1);
+    if (tiles > 0x3fffffffLL) return fail(NB_ERR_UNSUPPORTED, "too many tiles");
+    const long long workers = c.cg2 ? plan->sms / 2 : plan->sms;
+    const unsigned grid = (unsigned)((KIND == LIN_WEIGHT ? tiles : std::min(tiles, workers)) * (c.cg2 ? 2 : 1));
+    const bool wide = KIND != LIN_WEIGHT && c.bn % 128 == 0;
+#define NB_TL(T)                                                                                                                                       \
+    if (KIND == LIN_WEIGHT) return c.cg2 ? launch_tc<T, KIND, true, 32>(plan, P, grid, smem, st) : launch_tc<T, KIND, false, 32>(plan, P, grid, smem, st); \
+    if (wide) return c.cg2 ? launch_tc<T, KIND, true, 64>(plan, P, grid, smem, st) : launch_tc<T, KIND, false, 64>(plan, P, grid, smem, st);               \
+    return c.cg2 ? launch_tc<T, KIND, true, 32>(plan, P, grid, smem, st) : launch_tc<T, KIND, false, 32>(plan, P, grid, smem, st);
+    if (f16) { NB_TL(__half) }
+    NB_TL(__nv_bfloat16)
+#undef NB_TL
+}
+
+// ---------------------------------------------------------------- CUDA cores: launch
+template <typename T, int KIND> nb_status run_simt(const nb_linear_plan_s* plan, LinArgs& P, bool vec, void* workspace, cudaStream_t st) {
+    const SimtCfg c = simt_cfg(P.M, P.N, P.K, plan->sms, KIND == LIN_WEIGHT);
+    if (c.tiles > 0x7fffffffLL) return fail(NB_ERR_UNSUPPORTED, "too many tiles");
+    P.kslice = c.kslice;
+    P.slices = c.slices;
+    P.partial = static_cast<float*>(workspace);
+    const dim3 grid((unsigned)c.tiles, 1, (unsigned)c.slices);
+    if (vec) launch_k(lin_simt_kernel<T, KIND, true>, grid, dim3(LS_THREADS), 0, st, 1, P);
+    else launch_k(lin_simt_kernel<T, KIND, false>, grid, dim3(LS_THREADS), 0, st, 1, P);
+    NB_LAUNCH_OK("lin_simt");
+    if (KIND != LIN_WEIGHT && c.slices > 1) {
+        launch_k(lin_slices_kernel<T, KIND>, dim3((unsigned)std::min<long long>(ceil_div(P.M * P.N, 256), plan->sms * 8)), dim3(256), 0, st, 1, P);
+        NB_LAUNCH_OK("lin_slices");
+    }
+    return NB_OK;
+}
+template <int KIND> nb_status run_simt_any(const nb_linear_plan_s* plan, LinArgs& P, bool vec, void* workspace, cudaStream_t st) {
+    if (plan->d.dtype == NB_DTYPE_F32) return run_simt<float, KIND>(plan, P, vec, workspace, st);
+    if (plan->d.dtype == NB_DTYPE_BF16) return run_simt<__nv_bfloat16, KIND>(plan, P, vec, workspace, st);
+    return run_simt<__half, KIND>(plan, P, vec, workspace, st);
+}
+
+template <typename T> nb_status run_rows(const nb_linear_plan_s* plan, LinArgs& P, int rows, cudaStream_t st) {
+    // warps that share a column: enough warps for the GPU, but at least two 16-byte pieces a lane
+    int wpc = 1;
+    while (wpc < 8 && P.N * wpc < plan->sms * 16LL && P.K / (16 / (int)sizeof(T)) >= 64LL * 2 * wpc) wpc *= 2;
+    P.slices = 1;
+    const unsigned grid = (unsigned)ceil_div(P.N, LR_THREADS / 32 / wpc);
+    if (rows == 1) launch_k(lin_rows_kernel<T, 1>, dim3(grid), dim3(LR_THREADS), 0, st, 1, P, rows, wpc);
+    else if (rows == 2) launch_k(lin_rows_kernel<T, 2>, dim3(grid), dim3(LR_THREADS), 0, st, 1, P, rows, wpc);
+    else if (rows <= 4) launch_k(lin_rows_kernel<T, 4>, dim3(grid), dim3(LR_THREADS), 0, st, 1, P, rows, wpc);
+    else launch_k(lin_rows_kernel<T, 8>, dim3(grid), dim3(LR_THREADS), 0, st, 1, P, rows, wpc);
+    return launch_ok("lin_rows");
+}
+
+nb_status check_call(const nb_linear_plan_s* plan, int64_t rows) {
+    if (!plan) return fail(NB_ERR_INVALID_ARG, "plan is NULL");
+    if (rows <= 0) return fail(NB_ERR_INVALID_ARG, "rows must be positive");
+    if (rows >= 0x7fff0000LL) return fail(NB_ERR_UNSUPPORTED, "too many rows");
+    return NB_OK;
+}
+nb_status check_matrix(const char* name, const void* p, int64_t* ld, int64_t cols, size_t es) {
+    if (*ld == 0) *ld = cols;
+    if (*ld < cols) return fail(NB_ERR_INVALID_ARG, "the pitch of %s is smaller than its row", name);
+    if (reinterpret_cast<uintptr_t>(p) & (es - 1)) return fail(NB_ERR_ALIGNMENT, "%s is not aligned to its element size", name);
+    return NB_OK;
+}
+nb_status check16(const char* name, const void* p) {
+    if (reinterpret_cast<uintptr_t>(p) & 15u) return fail(NB_ERR_ALIGNMENT, "%s is not 16-byte aligned", name);
+    return NB_OK;
+}
+bool vec4(const void* q, long long ld, long long cols, size_t es) { return !(reinterpret_cast<uintptr_t>(q) & (4 * es - 1)) && ld % 4 == 0 && cols % 4 == 0; }
+
+}  // namespace
+
+extern "C" {
+
+nb_status nb_linear_plan_create(const nb_linear_desc* desc, int device, nb_linear_plan* out) {
+    g_err.clear();
+    if (!out) return fail(NB_ERR_INVALID_ARG, "out_plan is NULL");
+    *out = nullptr;
+    if (!desc) return fail(NB_ERR_INVALID_ARG, "desc is NULL");
+    if (desc->struct_size != sizeof(nb_linear_desc)) return fail(NB_ERR_INVALID_ARG, "nb_linear_desc.struct_size is %u, expected %zu", desc->struct_size, sizeof(nb_linear_desc));
+    if (desc->c_in <= 0 || desc->c_out <= 0 || desc->c_in > (1 << 24) || desc->c_out > (1 << 24)) return fail(NB_ERR_INVALID_ARG, "c_in and c_out must be in 1 .. 2^24");
+    if (desc->dtype != NB_DTYPE_F32 && desc->dtype != NB_DTYPE_BF16 && desc->dtype != NB_DTYPE_F16) return fail(NB_ERR_INVALID_ARG, "unknown dtype %d", desc->dtype);
+    if (desc->flags & ~NB_LINEAR_FLAG_FORCE_SIMT) return fail(NB_ERR_INVALID_ARG, "unknown flags %u", desc->flags);
+    int sms = 0, major = 0;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, device) != cudaSuccess) {
+        cudaGetLastError();
+        return fail(NB_ERR_CUDA, "cannot query device %d", device);
+    }
+    if (major != 10) return fail(NB_ERR_ARCH, "device %d is not compute capability 10.x", device);
+    std::unique_ptr<nb_linear_plan_s> p(new (std::nothrow) nb_linear_plan_s);
+    if (!p) return fail(NB_ERR_INTERNAL, "out of host memory");
+    p->d = *desc;
+    p->device = device;
+    p->sms = std::max(sms, 2);
+    DeviceGuard on_device(device);
+    NB_CUDA_CHECK(cudaMalloc(&p->status, ST_WORDS * sizeof(int)));
+    const cudaError_t e = cudaMemset(p->status, 0, ST_WORDS * sizeof(int));
+    if (e != cudaSuccess) {
+        cudaFree(p->status);
+        return fail(NB_ERR_CUDA, "cudaMemset failed: %s", cudaGetErrorString(e));
+    }
+    *out = p.release();
+    return NB_OK;
+}
+
+nb_status nb_linear_plan_destroy(nb_linear_plan p) {
+    g_err.clear();
+    if (!p) return NB_OK;
+    {
+        DeviceGuard on_device(p->device);
+        if (p->status) cudaFree(p->status);
+    }
+    delete p;
+    return NB_OK;
+}
+
+nb_status nb_linear_workspace_bytes(nb_linear_plan p, int64_t rows, size_t* bytes) {
+    g_err.clear();
+    NB_TRY(check_call(p, rows));
+    if (!bytes) return fail(NB_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = workspace_for(p, rows);
+    return NB_OK;
+}
+
+nb_status nb_linear_paths(nb_linear_plan p, int64_t rows, int32_t* paths3) {
+    g_err.clear();
+    NB_TRY(check_call(p, rows));
+    if (!paths3) return fail(NB_ERR_INVALID_ARG, "paths3 is NULL");
+    const int tc = tc_layer(p) ? 1 : 0;
+    paths3[0] = few_rows(p, rows) ? 2 : tc;
+    paths3[1] = paths3[2] = tc;
+    return NB_OK;
+}
+
+nb_status nb_linear_poll_status(nb_linear_plan p, void* stream) {
+    g_err.clear();
+    if (!p) return fail(NB_ERR_INVALID_ARG, "plan is NULL");
+    DeviceGuard on_device(p->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int host[ST_WORDS] = {0};
+    NB_CUDA_CHECK(cudaMemcpyAsync(host, p->status, sizeof host, cudaMemcpyDeviceToHost, st));
+    NB_CUDA_CHECK(cudaStreamSynchronize(st));
+    if (host[ST_ERR]) {
+        NB_CUDA_CHECK(cudaMemsetAsync(p->status, 0, sizeof host, st));
+        NB_CUDA_CHECK(cudaStreamSynchronize(st));
+        return fail((nb_status)host[ST_ERR], "a kernel gave up a bounded wait (site %d, block %d)", host[ST_WHERE], host[ST_DETAIL]);
+    }
+    return NB_OK;
+}
+
+nb_status nb_linear_fwd(nb_linear_plan p, int64_t rows, const void* x, int64_t ld_x, const void* w, const float* bias, int32_t act, const void* res, int64_t ld_res, void* z,
+                        void* out, int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream) {
+    g_err.clear();
+    NB_TRY(check_call(p, rows));
+    if (!x || !w || !out) return fail(NB_ERR_INVALID_ARG, "x, w and out must not be NULL");
+    if (act < NB_ACT_NONE || act > NB_ACT_GELU) return fail(NB_ERR_INVALID_ARG, "unknown act %d", act);
+    const size_t es = size_of(p->d.dtype);
+    const int64_t ci = p->d.c_in, co = p->d.c_out;
+    NB_TRY(check_matrix("x", x, &ld_x, ci, es));
+    NB_TRY(check_matrix("out", out, &ld_out, co, es));
+    if (res) NB_TRY(check_matrix("res", res, &ld_res, co, es));
+    NB_TRY(check16("w", w));
+    NB_TRY(check16("bias", bias));
+    if (reinterpret_cast<uintptr_t>(z) & (es - 1)) return fail(NB_ERR_ALIGNMENT, "z is not aligned to its element size");
+    NB_TRY(check_ws(workspace, workspace_bytes, workspace_for(p, rows)));
+    DeviceGuard on_device(p->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    LinArgs A;
+    memset(&A, 0, sizeof A);
+    A.a = x; A.lda = ld_x; A.b = w; A.ldb = ci;
+    A.M = rows; A.N = co; A.K = ci;
+    A.bias = bias; A.act = act; A.add = res; A.ld_add = ld_res; A.z = z; A.out = out; A.ld_out = ld_out;
+    if (few_rows(p, rows) && whole16(x, ld_x, es)) {
+        if (p->d.dtype == NB_DTYPE_F32) return run_rows<float>(p, A, (int)rows, st);
+        if (p->d.dtype == NB_DTYPE_BF16) return run_rows<__nv_bfloat16>(p, A, (int)rows, st);
+        return run_rows<__half>(p, A, (int)rows, st);
+    }
+    if (tc_layer(p) && whole16(x, ld_x, es) && whole16(out, ld_out, es) && (!res || whole16(res, ld_res, es)) && whole16(z, co, es)) {
+        const TlCfg c = choose_rows(rows, co, ci, p->sms, 6.0 + (act ? 10.0 : 0.0) + (z ? 3.0 : 0.0) + (res ? 3.0 : 0.0));
+        TcLinParams P;
+        memset(&P, 0, sizeof P);
+        P.M = (int)rows; P.N = (int)co;
+        P.bias = bias; P.act = act; P.add = res; P.ld_add = ld_res; P.want_z = z != nullptr;
+        const int np = c.bn % 128 == 0 ? 64 : 32;
+        if (!encode2(&P.tmA, p->d.dtype, x, rows, ci, ld_x, 64, 128, true) || !encode2(&P.tmB, p->d.dtype, w, co, ci, ci, 64, c.cg2 ? c.bn / 2 : c.bn, true) ||
+            !encode2(&P.tmOut, p->d.dtype, out, rows, co, ld_out, np, 32, false) || (z && !encode2(&P.tmZ, p->d.dtype, z, rows, co, co, np, 32, false)))
+            return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+        return run_tc<LIN_FWD>(p, c, P, st);
+    }
+    return run_simt_any<LIN_FWD>(p, A, vec4(x, ld_x, ci, es) && vec4(w, ci, ci, es), workspace, st);
+}
+
+nb_status nb_linear_bwd_data(nb_linear_plan p, int64_t rows, const void* dy, int64_t ld_dy, const void* w, const void* z_in, int32_t act_in, const void* add, int64_t ld_add,
+                             void* dx, int64_t ld_dx, void* workspace, size_t workspace_bytes, void* stream) {
+    g_err.clear();
+    NB_TRY(check_call(p, rows));
+    if (!dy || !w || !dx) return fail(NB_ERR_INVALID_ARG, "dy, w and dx must not be NULL");
+    if (act_in < NB_ACT_NONE || act_in > NB_ACT_GELU) return fail(NB_ERR_INVALID_ARG, "unknown act_in %d", act_in);
+    if ((act_in == NB_ACT_NONE) != !z_in) return fail(NB_ERR_INVALID_ARG, "z_in must be NULL exactly when act_in is NB_ACT_NONE");
+    const size_t es = size_of(p->d.dtype);
+    const int64_t ci = p->d.c_in, co = p->d.c_out;
+    NB_TRY(check_matrix("dy", dy, &ld_dy, co, es));
+    NB_TRY(check_matrix("dx", dx, &ld_dx, ci, es));
+    if (add) NB_TRY(check_matrix("add", add, &ld_add, ci, es));
+    NB_TRY(check16("w", w));
+    if (reinterpret_cast<uintptr_t>(z_in) & (es - 1)) return fail(NB_ERR_ALIGNMENT, "z_in is not aligned to its element size");
+    NB_TRY(check_ws(workspace, workspace_bytes, workspace_for(p, rows)));
+    DeviceGuard on_device(p->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (tc_layer(p) && whole16(dy, ld_dy, es) && whole16(dx, ld_dx, es) && (!add || whole16(add, ld_add, es)) && whole16(z_in, ci, es)) {
+        const TlCfg c = choose_rows(rows, ci, co, p->sms, 6.0 + (z_in ? 16.0 : 0.0) + (add ? 3.0 : 0.0));
+        TcLinParams P;
+        memset(&P, 0, sizeof P);
+        P.M = (int)rows; P.N = (int)ci;
+        P.act = act_in; P.add = add; P.ld_add = ld_add; P.zin = z_in;
+        const int np = c.bn % 128 == 0 ? 64 : 32;
+        if (!encode2(&P.tmA, p->d.dtype, dy, rows, co, ld_dy, 64, 128, true) || !encode2(&P.tmB, p->d.dtype, w, co, ci, ci, 64, TL_KC, true) ||
+            !encode2(&P.tmOut, p->d.dtype, dx, rows, ci, ld_dx, np, 32, false))
+            return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+        return run_tc<LIN_DATA>(p, c, P, st);
+    }
+    LinArgs A;
+    memset(&A, 0, sizeof A);
+    A.a = dy; A.lda = ld_dy; A.b = w; A.ldb = ci;
+    A.M = rows; A.N = ci; A.K = co;
+    A.act = act_in; A.zin = z_in; A.add = add; A.ld_add = ld_add; A.out = dx; A.ld_out = ld_dx;
+    return run_simt_any<LIN_DATA>(p, A, vec4(dy, ld_dy, co, es) && vec4(w, ci, ci, es), workspace, st);
+}
+
+nb_status nb_linear_bwd_weight(nb_linear_plan p, int64_t rows, const void* x, int64_t ld_x, const void* dy, int64_t ld_dy, float* dw, float* dbias, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+    g_err.clear();
+    NB_TRY(check_call(p, rows));
+    if (!x || !dy || !dw) return fail(NB_ERR_INVALID_ARG, "x, dy and dw must not be NULL");
+    const size_t es = size_of(p->d.dtype);
+    const int64_t ci = p->d.c_in, co = p->d.c_out;
+    NB_TRY(check_matrix("x", x, &ld_x, ci, es));
+    NB_TRY(check_matrix("dy", dy, &ld_dy, co, es));
+    NB_TRY(check16("dw", dw));
+    NB_TRY(check16("dbias", dbias));
+    NB_TRY(check_ws(workspace, workspace_bytes, workspace_for(p, rows)));
+    DeviceGuard on_device(p->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    const long long n1 = co * ci;
+    auto sums = [&](const float* p1, int s1, const float* p2, int s2) -> nb_status {
+        const long long work = std::max(s1 ? ceil_div(n1, n1 % 4 ? 1 : 4) : 0LL, s2 ? (long long)co : 0LL);
+        launch_k(lin_weight_sums_kernel, dim3((unsigned)std::min<long long>(ceil_div(work, 256), p->sms * 8)), dim3(256), 0, st, 1, p1, s1, n1, dw, p2, s2, (int)co, dbias);
+        return launch_ok("lin_weight_sums");
+    };
+    if (tc_layer(p) && whole16(x, ld_x, es) && whole16(dy, ld_dy, es)) {
+        const TlCfg c = choose_weight(co, ci, rows, p->sms);
+        TcLinParams P;
+        memset(&P, 0, sizeof P);
+        P.M = (int)co; P.N = (int)ci;
+        float* part = c.splits > 1 ? reinterpret_cast<float*>(ws) : dw;
+        float* db = reinterpret_cast<float*>(ws + (c.splits > 1 ? align_up((size_t)c.splits * n1 * 4, 256) : 0));
+        const int db_parts = c.splits * c.n_tiles;
+        if (dbias && db_parts == 1) db = dbias;
+        P.db = dbias ? db : nullptr;
+        const cuuint64_t dims[3] = {(cuuint64_t)ci, (cuuint64_t)co, (cuuint64_t)c.splits}, strides[2] = {(cuuint64_t)ci * 4, (cuuint64_t)n1 * 4};
+        const cuuint32_t box[3] = {32, 32, 1};
+        if (!encode2(&P.tmA, p->d.dtype, dy, rows, co, ld_dy, 64, TL_KC, true) || !encode2(&P.tmB, p->d.dtype, x, rows, ci, ld_x, 64, TL_KC, true) ||
+            !encode(&P.tmOut, NB_DTYPE_F32, part, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, false))
+            return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+        NB_TRY(run_tc<LIN_WEIGHT>(p, c, P, st));
+        const bool add_db = dbias && db_parts > 1;
+        return c.splits > 1 || add_db ? sums(part, c.splits > 1 ? c.splits : 0, db, add_db ? db_parts : 0) : NB_OK;
+    }
+    LinArgs A;
+    memset(&A, 0, sizeof A);
+    A.a = dy; A.lda = ld_dy; A.b = x; A.ldb = ld_x;
+    A.M = co; A.N = ci; A.K = rows;
+    A.out = dw; A.ld_out = ci;
+    NB_TRY(run_simt_any<LIN_WEIGHT>(p, A, vec4(dy, ld_dy, co, es) && vec4(x, ld_x, ci, es), workspace, st));
+    const int slices = A.slices;
+    float* db = reinterpret_cast<float*>(ws + (slices > 1 ? align_up((size_t)slices * n1 * 4, 256) : 0));
+    int parts = 0;
+    if (dbias) {
+        const long long per = ceil_div(rows, colsum_parts(rows));
+        parts = (int)ceil_div(rows, per);
+        const dim3 grid((unsigned)ceil_div(co, 32), (unsigned)parts);
+        if (p->d.dtype == NB_DTYPE_F32) launch_k(lin_colsum_kernel<float>, grid, dim3(256), 0, st, 1, static_cast<const float*>(dy), (long long)ld_dy, (long long)rows, (int)co, per, db);
+        else if (p->d.dtype == NB_DTYPE_BF16)
+            launch_k(lin_colsum_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, 1, static_cast<const __nv_bfloat16*>(dy), (long long)ld_dy, (long long)rows, (int)co, per, db);
+        else launch_k(lin_colsum_kernel<__half>, grid, dim3(256), 0, st, 1, static_cast<const __half*>(dy), (long long)ld_dy, (long long)rows, (int)co, per, db);
+        NB_LAUNCH_OK("lin_colsum");
+    }
+    return slices > 1 || parts ? sums(static_cast<const float*>(workspace), slices > 1 ? slices : 0, db, parts) : NB_OK;
+}
+
+nb_status nb_act_bwd(int32_t dtype, int64_t n, int32_t act, const void* dy, const void* z, void* dz, void* stream) {
+    g_err.clear();
+    if (dtype != NB_DTYPE_F32 && dtype != NB_DTYPE_BF16 && dtype != NB_DTYPE_F16) return fail(NB_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+    if (n <= 0) return fail(NB_ERR_INVALID_ARG, "n must be positive");
+    if (act != NB_ACT_SILU && act != NB_ACT_GELU) return fail(NB_ERR_INVALID_ARG, "act %d has no gradient pass", act);
+    if (!dy || !z || !dz) return fail(NB_ERR_INVALID_ARG, "dy, z and dz must not be NULL");
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(dy) | reinterpret_cast<uintptr_t>(z) | reinterpret_cast<uintptr_t>(dz);
+    if (bits & (size_of(dtype) - 1)) return fail(NB_ERR_ALIGNMENT, "a pointer is not aligned to its element size");
+    const bool vec = !(bits & 15u);
+    int dev = 0, sms = 148;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const long long items = vec ? ceil_div(n, 16 / (long long)size_of(dtype)) : n;
+    const dim3 grid((unsigned)std::min<long long>(ceil_div(items, 256), sms * 16LL));
+#define NB_ACTB(T)                                                                                                                                           \
+    if (vec) launch_k(lin_act_bwd_kernel<T, true>, grid, dim3(256), 0, st, 1, static_cast<const T*>(dy), static_cast<const T*>(z), static_cast<T*>(dz), (long long)n, (int)act); \
+    else launch_k(lin_act_bwd_kernel<T, false>, grid, dim3(256), 0, st, 1, static_cast<const T*>(dy), static_cast<const T*>(z), static_cast<T*>(dz), (long long)n, (int)act);
+    if (dtype == NB_DTYPE_F32) { NB_ACTB(float) }
+    else if (dtype == NB_DTYPE_BF16) { NB_ACTB(__nv_bfloat16) }
+    else { NB_ACTB(__half) }
+#undef NB_ACTB
+    return launch_ok("lin_act_bwd");
+}
+
+}  // extern "C"

@@ -18,6 +18,7 @@
 #include "common.cuh"
 #include "ptx_sm100.cuh"
 #include "simt_conv.cuh"
+#include "tc_common.cuh"
 
 namespace nbcbs {
 
@@ -110,39 +111,6 @@ template <bool HALF> __device__ __forceinline__ int igemm_first_kblock(const Ige
 constexpr int TC_BM = 128;
 constexpr int IG_THREADS = 384;  // implicit-GEMM kernel: the roles below plus a second epilogue team in warps 7-10 and a second MMA issuer in warp 11
 
-__device__ __forceinline__ uint64_t global_timer_ns() {
-    uint64_t t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
-
-// Bounded mbarrier wait: gives up after `limit_ns` (or as soon as another role has given up), records the site.
-__device__ __noinline__ bool wait_bar(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status, int site, uint64_t limit_ns = kWaitLimitNs) {
-    uint64_t t0 = 0;
-    for (uint32_t i = 0;; ++i) {
-        if (ptx::mbar_try_wait_parked(bar, parity, 4000u)) return true;
-        if ((i & 127u) == 127u) {
-            if (*abort_flag) return false;
-            const uint64_t now = global_timer_ns();
-            if (t0 == 0) {
-                t0 = now;
-            } else if (now - t0 > limit_ns) {
-                *abort_flag = 1;
-                report_timeout(status, site, (int)blockIdx.x);
-                return false;
-            }
-        }
-    }
-}
-
-// Fast path inline (the barrier is usually complete already), slow bounded path out of line.
-// Called by all 32 lanes of a producer or MMA warp; the lanes leave together with the same answer.
-__device__ __forceinline__ bool wait_bar_fast(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status, int site) {
-    bool ok = ptx::mbar_try_wait(bar, parity);
-    if (!ok) ok = wait_bar(bar, parity, abort_flag, status, site);
-    return __all_sync(0xffffffffu, ok) != 0;
-}
-
 // Barriers over the 256 threads of a kernel's two epilogue teams, the second with the AND of a predicate, so that all of them take
 // the same decision.
 __device__ __forceinline__ void epi2_bar_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
@@ -160,20 +128,6 @@ __device__ __forceinline__ bool epi2_bar_and(bool ok) {
         : "memory");
     return r != 0;
 }
-template <typename OutT> __device__ __forceinline__ uint32_t pack2(float a, float b, int* sat);
-template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b, int*) {
-    __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<uint32_t*>(&v);
-}
-// fp16 stores saturate to the largest finite value; `sat` collects, per 16-bit half, a flag bit (bit 15 / 31) that is set
-// when a stored magnitude is 65504 (0x7bff) or an exceptional pattern above it.
-template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b, int* sat) {
-    uint32_t v;
-    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(b), "f"(a));
-    if (sat) *sat |= (int)((v & 0x7fff7fffu) + 0x04010401u);  // (sat is a compile-time NULL where the caller tracks saturation otherwise)
-    return v;
-}
-
 // One epilogue pass of NP columns (16, 32, 48 or 64) by one warp when the output goes through TMA: this thread's
 // accumulator row segment travels TMEM -> registers -> dense staging rows (row pitch NP*2 bytes; 128-byte rows in the
 // 128-byte swizzle), `release` is called as soon as the registers hold the data (the accumulator may be reused), lane 0
@@ -825,43 +779,10 @@ struct TcPlan {
 
 namespace tcdetail {
 
-inline std::string& err() {
-    static thread_local std::string e;
-    return e;
-}
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-typedef CUresult (*EncodeIm2colFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const int*, const int*,
-                                   cuuint32_t, cuuint32_t, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                   CUtensorMapFloatOOBfill);
-
-struct DriverFns {
-    EncodeTiledFn tiled = nullptr;
-    EncodeIm2colFn im2col = nullptr;
-    bool tried = false;
-};
-inline DriverFns& driver() {
-    static DriverFns d;
-    if (!d.tried) {
-        d.tried = true;
-        void* f = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
-            d.tiled = reinterpret_cast<EncodeTiledFn>(f);
-        f = nullptr;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeIm2col", &f, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
-            d.im2col = reinterpret_cast<EncodeIm2colFn>(f);
-    }
-    return d;
-}
-
 inline CUtensorMapSwizzle tma_swizzle_for(int KC) {
     return KC == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : KC == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B;
 }
 inline uint32_t umma_swizzle_for(int KC) { return KC == 64 ? (uint32_t)ptx::kSwizzle128 : KC == 32 ? (uint32_t)ptx::kSwizzle64 : (uint32_t)ptx::kSwizzle32; }
-
-constexpr size_t kMaxSmem = 232448;  // 227 KB opt-in limit per CTA
 
 // Tile configuration for a GEMM with M rows, `rowsB` output channels, `ntaps` taps of `Ca` channels each.
 // Measured on B200: a tcgen05.mma of 128 x N x 16 takes max(97, N/2) cycles, so N below 192 wastes the tensor pipe;

@@ -1,0 +1,436 @@
+// Matrix products of MLP layers on the tensor cores (see include/nb_linear.h): D[m][n] = sum_k A(m,k) B(n,k) with 16-bit operands,
+// fetched by TMA in the 128-byte swizzle, multiplied by tcgen05.mma into fp32 accumulators in TMEM and finished by eight
+// epilogue warps.
+//   LIN_FWD     m = row,   n = c_out, k = c_in    A = x  (k contiguous: K-major),  B = w (K-major)
+//   LIN_DATA    m = row,   n = c_in,  k = c_out   A = dy (K-major),                B = w (n contiguous: MN-major)
+//   LIN_WEIGHT  m = c_out, n = c_in,  k = row     A = dy (m contiguous: MN-major), B = x (MN-major)
+// No operand is rearranged in memory.  Tiles are 128 x BN a CTA or, with CG2, 256 x BN a pair of CTAs (cta_group::2: each has 128
+// rows and fetches its own rows of A and half of B); the forward and data-gradient kernels are persistent, with two accumulator
+// sets so that the epilogue of a tile runs beside the products of the next; the weight gradient gives every tile a slice of the
+// rows and adds the slices in a second kernel.  No multicast; every wait on an mbarrier is bounded.
+#pragma once
+#include "linear.cuh"
+#include "tc_common.cuh"
+
+namespace nbcbs {
+
+constexpr int TL_THREADS = 320;  // warp 0: TMA producer, warp 1: MMA issuer and owner of TMEM, warps 2-9: epilogue
+constexpr int TL_KC = 64;        // k of a stage: 128 bytes of a 16-bit K-major operand
+constexpr uint32_t TL_BLK = 64 * 128;         // an MN-major block: 64 m (or n) by 64 k
+constexpr uint32_t TL_A_BYTES = 128 * 128;    // A rows of a CTA by 64 k
+constexpr int TL_STG = 4096;                  // staging buffer of an epilogue warp: 32 rows of 128 bytes
+constexpr uint32_t TL_ONES_BYTES = 4096;
+
+struct TcLinParams {
+    CUtensorMap tmA, tmB, tmOut, tmZ;
+    int M, N, kblocks;  // k-blocks of TL_KC
+    int BN, m_tiles, n_tiles, group_m;
+    int stages, bufs, acc_stride;  // bufs: staging buffers of an epilogue warp (1 or 2)
+    int nblkB;                     // MN-major: 64-column blocks of this CTA's part of B
+    uint32_t b_bytes, idesc;
+    // epilogue
+    const float* bias;
+    int act;
+    const void *add, *zin;
+    long long ld_add;
+    int want_z;
+    // weight gradient
+    int splits, kb_per_split;
+    float* db;  // partial sums of dbias [splits * n_tiles][M], or NULL
+    uint32_t idesc_ones;
+    int* status;
+};
+
+// Order of the tiles: group_m row tiles by all column tiles at a time, so that what is in flight at once shares both operands in L2.
+__device__ __forceinline__ void tl_tile(const TcLinParams& p, int tile, int& mt, int& nt) {
+    const int per = p.group_m * p.n_tiles, g = tile / per, r = tile - g * per;
+    const int first = g * p.group_m, rows = min(p.group_m, p.m_tiles - first);
+    nt = r / rows;
+    mt = first + r - nt * rows;
+}
+
+// Eight consecutive 16-bit elements as four pairs.
+template <typename T> __device__ __forceinline__ float2 tl_pair(const uint4& v, int j) {
+    const uint32_t w = j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w;
+    return pair_to_f32<T>(reinterpret_cast<const T*>(&w));
+}
+
+// One pass of the epilogue by a warp: NP (32 or 64) accumulator columns of its 32 rows become results, go through the warp's
+// staging rows (rows of NP*2 bytes in the swizzle of that width) and leave as a TMA store.
+template <typename T, int KIND, int NP> struct TlPass {
+    uint4 ad[NP / 8], zi[NP / 8];  // this row's pieces of `add` and of z_in, requested before the accumulators are waited for
+    __device__ __forceinline__ void request(const TcLinParams& p, long long row, int col) {
+        const bool live = row < p.M;
+#pragma unroll
+        for (int j = 0; j < NP / 8; ++j) {
+            const bool in = live && col + 8 * j < p.N;
+            if (p.add) ad[j] = in ? *reinterpret_cast<const uint4*>(static_cast<const T*>(p.add) + row * p.ld_add + col + 8 * j) : make_uint4(0u, 0u, 0u, 0u);
+            if (KIND == LIN_DATA && p.zin) zi[j] = in ? *reinterpret_cast<const uint4*>(static_cast<const T*>(p.zin) + row * p.N + col + 8 * j) : make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+    static __device__ __forceinline__ int slot(int lane, int j) { return NP == 64 ? (j ^ (lane & 7)) : (j ^ ((lane >> 1) & 3)); }
+    static __device__ __forceinline__ void stage(uint8_t* my_row, int lane, const float2 (&v)[NP / 2]) {
+#pragma unroll
+        for (int j = 0; j < NP / 8; ++j) {
+            uint4 o;
+            o.x = pack2<T>(v[4 * j].x, v[4 * j].y, nullptr);
+            o.y = pack2<T>(v[4 * j + 1].x, v[4 * j + 1].y, nullptr);
+            o.z = pack2<T>(v[4 * j + 2].x, v[4 * j + 2].y, nullptr);
+            o.w = pack2<T>(v[4 * j + 3].x, v[4 * j + 3].y, nullptr);
+            *reinterpret_cast<uint4*>(my_row + slot(lane, j) * 16) = o;
+        }
+    }
+    template <class Release, class Buffer>
+    __device__ __forceinline__ void finish(const TcLinParams& p, uint32_t taddr, int lane, int row0, int col, Release release, Buffer buffer) {
+        uint32_t r[NP];
+#pragma unroll
+        for (int h = 0; h < NP / 32; ++h) ptx::tmem_ld_32x32b_x32(taddr + 32u * h, r + 32 * h);
+        ptx::tmem_ld_wait();
+        release();
+        float2 v[NP / 2];
+#pragma unroll
+        for (int j = 0; j < NP / 2; ++j) v[j] = make_float2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+        if (KIND == LIN_FWD) {
+            if (p.bias) {
+#pragma unroll
+                for (int j = 0; j < NP / 4; ++j) {
+                    const float4 b = col + 4 * j < p.N ? __ldg(reinterpret_cast<const float4*>(p.bias + col + 4 * j)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    v[2 * j] = add2(v[2 * j], make_float2(b.x, b.y));
+                    v[2 * j + 1] = add2(v[2 * j + 1], make_float2(b.z, b.w));
+                }
+            }
+            if (p.want_z) {
+                uint8_t* stg = buffer();
+                stage(stg + lane * (NP * 2), lane, v);
+                ptx::fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    ptx::tma_store_2d(&p.tmZ, stg, col, row0);
+                    ptx::tma_store_commit();
+                }
+            }
+            if (p.act == NB_ACT_GELU) {
+#pragma unroll
+                for (int j = 0; j < NP / 2; ++j) v[j] = lin_act2(v[j], NB_ACT_GELU);
+            } else if (p.act == NB_ACT_SILU) {
+#pragma unroll
+                for (int j = 0; j < NP / 2; ++j) v[j] = lin_act2(v[j], NB_ACT_SILU);
+            }
+        }
+        if (p.add) {
+#pragma unroll
+            for (int j = 0; j < NP / 2; ++j) v[j] = add2(v[j], tl_pair<T>(ad[j / 4], j & 3));
+        }
+        if (KIND == LIN_DATA && p.zin) {
+            if (p.act == NB_ACT_GELU) {
+#pragma unroll
+                for (int j = 0; j < NP / 2; ++j) v[j] = mul2(v[j], lin_act_grad2(tl_pair<T>(zi[j / 4], j & 3), NB_ACT_GELU));
+            } else {
+#pragma unroll
+                for (int j = 0; j < NP / 2; ++j) v[j] = mul2(v[j], lin_act_grad2(tl_pair<T>(zi[j / 4], j & 3), NB_ACT_SILU));
+            }
+        }
+        uint8_t* stg = buffer();
+        stage(stg + lane * (NP * 2), lane, v);
+        ptx::fence_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            ptx::tma_store_2d(&p.tmOut, stg, col, row0);
+            ptx::tma_store_commit();
+        }
+        __syncwarp();  // (the next accumulator load wants the whole warp)
+    }
+};
+
+template <typename T, int KIND, bool CG2, int NP> __global__ void __launch_bounds__(TL_THREADS, 1) tc_linear_kernel(const __grid_constant__ TcLinParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t* sA = smem;
+    uint8_t* sB = sA + (size_t)p.stages * TL_A_BYTES;
+    uint8_t* stg = sB + (size_t)p.stages * p.b_bytes;              // [8 warps][bufs][TL_STG]
+    uint8_t* ones = stg + (size_t)8 * p.bufs * TL_STG;             // weight gradient with dbias
+    uint64_t* bars = reinterpret_cast<uint64_t*>(ones + (KIND == LIN_WEIGHT ? TL_ONES_BYTES : 0));
+    uint64_t* full = bars;
+    uint64_t* empty = full + p.stages;
+    uint64_t* tfull = empty + p.stages;  // [2]
+    uint64_t* tempty = tfull + 2;        // [2]
+    uint64_t* drain = tempty + 2;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    constexpr bool A_MN = KIND == LIN_WEIGHT, B_MN = KIND != LIN_FWD;
+
+    pdl_launch_dependents();
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const uint32_t rank = CG2 ? (blockIdx.x & 1u) : 0u;
+    const int worker = CG2 ? (int)(blockIdx.x >> 1) : (int)blockIdx.x, nworkers = CG2 ? (int)(gridDim.x >> 1) : (int)gridDim.x;
+    const int tiles = p.m_tiles * p.n_tiles * (KIND == LIN_WEIGHT ? p.splits : 1);
+    constexpr int TM = CG2 ? 256 : 128;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            ptx::mbar_init(full + s, 1);
+            ptx::mbar_init(empty + s, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            ptx::mbar_init(tfull + i, 1);
+            ptx::mbar_init(tempty + i, CG2 ? 16 : 8);  // one arrival per epilogue warp (of both CTAs)
+        }
+        ptx::mbar_init(drain, 1);
+        *abort_flag = 0;
+        ptx::fence_mbar_init();
+    }
+    if (lane == 0 && warp == 0) {
+        ptx::prefetch_tmap(&p.tmA);
+        ptx::prefetch_tmap(&p.tmB);
+    }
+    if (lane == 0 && warp == 2) ptx::prefetch_tmap(&p.tmOut);
+    if (KIND == LIN_WEIGHT && p.db && warp >= 2) {
+        // 16 columns of ones as an operand: the same whatever the layout
+        const uint32_t w = (p.idesc >> 7) & 1u ? 0x3f803f80u : 0x3c003c00u;  // (bf16 or fp16, as the descriptor says)
+        for (uint32_t i = threadIdx.x - 64; i < TL_ONES_BYTES / 4; i += 256) reinterpret_cast<uint32_t*>(ones)[i] = w;
+        ptx::fence_async_smem();
+    }
+    if (warp == 1) {
+        if (CG2) {
+            ptx::tmem_alloc_cg2(tmem_slot, 512);
+            ptx::tmem_relinquish_cg2();
+        } else {
+            ptx::tmem_alloc(tmem_slot, 512);
+            ptx::tmem_relinquish();
+        }
+    }
+    ptx::tc_fence_before();
+    if (CG2) ptx::cluster_sync_all(); else __syncthreads();  // barriers of both CTAs are initialised before any remote arrive
+    ptx::tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    // a work item: a tile and, for the weight gradient, a slice of the rows
+    auto item = [&](int i, int& mt, int& nt, int& split, int& kb0, int& kb1) {
+        split = 0;
+        if (KIND == LIN_WEIGHT) {  // slices fastest: what runs at once reads different rows of all channels
+            split = i % p.splits;
+            i /= p.splits;
+        }
+        tl_tile(p, i, mt, nt);
+        kb0 = KIND == LIN_WEIGHT ? split * p.kb_per_split : 0;
+        kb1 = KIND == LIN_WEIGHT ? min(p.kblocks, kb0 + p.kb_per_split) : p.kblocks;
+    };
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ TMA producer (the warp runs converged, `leader` issues)
+        const uint32_t leader = ptx::elect_one() ? 1u : 0u;
+        int s = 0;
+        uint32_t ph = 0;
+        long long issued = 0;
+        bool ok = true;
+        const int bn_own = CG2 ? p.BN / 2 : p.BN;
+        const uint32_t a_u32 = ptx::smem_u32(sA), b_u32 = ptx::smem_u32(sB);
+        const uint32_t full_u32 = CG2 ? ptx::mapa_u32(ptx::smem_u32(full), 0u) : ptx::smem_u32(full);  // pairs: counted at rank 0
+        const uint32_t tx = TL_A_BYTES + (B_MN ? (uint32_t)p.nblkB * TL_BLK : (uint32_t)bn_own * 128u);
+        auto load = [&](uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1) {
+            if (CG2) ptx::tma_load_2d_cg2_if(leader, dst, tm, bar, c0, c1); else ptx::tma_load_2d_u32_if(leader, dst, tm, bar, c0, c1);
+        };
+        pdl_wait();
+        for (int i = worker; ok && i < tiles; i += nworkers) {
+            int mt, nt, split, kb0, kb1;
+            item(i, mt, nt, split, kb0, kb1);
+            const int m0 = mt * TM + (int)rank * 128, n0 = nt * p.BN + (int)rank * bn_own;
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (!wait_bar_fast(empty + s, ph ^ 1u, abort_flag, p.status, 21)) {
+                    ok = false;
+                    break;
+                }
+                const uint32_t bar = full_u32 + 8u * (uint32_t)s, a = a_u32 + (uint32_t)s * TL_A_BYTES, b = b_u32 + (uint32_t)s * p.b_bytes;
+                if (!CG2) ptx::mbar_expect_tx_u32_if(leader, bar, tx);
+                else if (rank == 0) ptx::mbar_expect_tx_u32_if(leader, ptx::smem_u32(full) + 8u * (uint32_t)s, 2u * tx);
+                const int k = kb * TL_KC;
+                if (A_MN) {
+                    load(a, &p.tmA, bar, m0, k);
+                    load(a + TL_BLK, &p.tmA, bar, m0 + 64, k);
+                } else {
+                    load(a, &p.tmA, bar, k, m0);
+                }
+                if (B_MN) {
+                    for (int j = 0; j < p.nblkB; ++j) load(b + (uint32_t)j * TL_BLK, &p.tmB, bar, n0 + 64 * j, k);
+                } else {
+                    load(b, &p.tmB, bar, k, n0);
+                }
+                ++issued;
+                if (++s == p.stages) {
+                    s = 0;
+                    ph ^= 1u;
+                }
+            }
+        }
+        if (!ok) {
+            // Gave up: wait (bounded) for the loads still in flight so that nothing lands after the CTA has exited.
+            const int back = issued < (long long)p.stages ? (int)issued : p.stages;
+            for (int b = 0; b < back; ++b) {
+                s = (s == 0) ? p.stages - 1 : s - 1;
+                if (s == p.stages - 1) ph ^= 1u;
+                for (int j = 0; j < 100000 && !ptx::mbar_try_wait(full + s, ph); ++j) {
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer (in a pair that of rank 0)
+        const uint32_t leader = ptx::elect_one() ? 1u : 0u;
+        if (rank == 0) {
+            int s = 0, acc = 0;
+            uint32_t ph = 0, acc_ph = 0;
+            bool ok = true;
+            // K-major: rows of 128 bytes, 8 rows a group (SBO 1024), a K = 16 step is 32 bytes.  MN-major: 8 k rows of 128 bytes a group
+            // (SBO 1024), the next 64 m (n) one block behind (LBO), a K = 16 step is two groups.
+            const uint64_t da0 = ptx::make_smem_desc(ptx::smem_u32(sA), A_MN ? TL_BLK : 16u, 1024, ptx::kSwizzle128);
+            const uint64_t db0 = ptx::make_smem_desc(ptx::smem_u32(sB), B_MN ? TL_BLK : 16u, 1024, ptx::kSwizzle128);
+            const uint64_t d1 = KIND == LIN_WEIGHT ? ptx::make_smem_desc(ptx::smem_u32(ones), TL_BLK, 1024, ptx::kSwizzle128) : 0ull;
+            constexpr uint64_t ka = A_MN ? 128 : 2, kb_ = B_MN ? 128 : 2;
+            const uint64_t a_stage = TL_A_BYTES >> 4, b_stage = p.b_bytes >> 4;
+            const uint32_t empty_u32 = ptx::smem_u32(empty), tfull_u32 = ptx::smem_u32(tfull);
+            auto mma = [&](uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+                if (CG2) ptx::umma_f16_cg2_if(leader, d, a, b, idesc, accumulate); else ptx::umma_f16_if(leader, d, a, b, idesc, accumulate);
+            };
+            uint64_t da = da0, db = db0;
+            for (int i = worker; ok && i < tiles; i += nworkers) {
+                int mt, nt, split, kb0, kb1;
+                item(i, mt, nt, split, kb0, kb1);
+                if (!wait_bar_fast(tempty + acc, acc_ph ^ 1u, abort_flag, p.status, 22)) break;
+                ptx::tc_fence_after();
+                const uint32_t dt = tmem_base + (uint32_t)(acc * p.acc_stride);
+                uint32_t accumulate = 0, accumulate1 = 0;
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (!wait_bar_fast(full + s, ph, abort_flag, p.status, 23)) {
+                        ok = false;
+                        break;
+                    }
+                    ptx::tc_fence_after();
+                    mma(dt, da, db, p.idesc, accumulate);
+                    mma(dt, da + ka, db + kb_, p.idesc, 1u);
+                    mma(dt, da + 2 * ka, db + 2 * kb_, p.idesc, 1u);
+                    mma(dt, da + 3 * ka, db + 3 * kb_, p.idesc, 1u);
+                    accumulate = 1u;
+                    if (KIND == LIN_WEIGHT && p.db && kb % p.n_tiles == nt) {
+                        // sums of A over k: a product with columns of ones, whose share each column tile takes of the k-blocks in turn
+                        mma(dt + (uint32_t)p.BN, da, d1, p.idesc_ones, accumulate1);
+                        mma(dt + (uint32_t)p.BN, da + ka, d1, p.idesc_ones, 1u);
+                        mma(dt + (uint32_t)p.BN, da + 2 * ka, d1, p.idesc_ones, 1u);
+                        mma(dt + (uint32_t)p.BN, da + 3 * ka, d1, p.idesc_ones, 1u);
+                        accumulate1 = 1u;
+                    }
+                    if (CG2) ptx::umma_commit_cg2_mc_if(leader, empty_u32 + 8u * (uint32_t)s, 3); else ptx::umma_commit_u32_if(leader, empty_u32 + 8u * (uint32_t)s);
+                    da += a_stage;
+                    db += b_stage;
+                    if (++s == p.stages) {
+                        s = 0;
+                        ph ^= 1u;
+                        da = da0;
+                        db = db0;
+                    }
+                }
+                if (!ok) break;
+                if (CG2) ptx::umma_commit_cg2_mc_if(leader, tfull_u32 + 8u * (uint32_t)acc, 3); else ptx::umma_commit_u32_if(leader, tfull_u32 + 8u * (uint32_t)acc);
+                acc ^= 1;
+                if (acc == 0) acc_ph ^= 1u;
+            }
+            // Make sure every MMA issued by this thread has retired before TMEM is released.
+            if (CG2) ptx::umma_commit_cg2_if(leader, ptx::smem_u32(drain)); else ptx::umma_commit_u32_if(leader, ptx::smem_u32(drain));
+            for (int j = 0; j < 4000000 && !ptx::mbar_try_wait(drain, 0); ++j) {
+            }
+        }
+    } else {
+        // ------------------------------------------------------------------ epilogue: two teams of four warps, each half of the columns
+        const int ew = warp - 2, team = ew >> 2, lane_group = warp & 3;  // TMEM lanes [32*lane_group, +32)
+        const int ncol = p.BN / 2, c_lo = team * ncol;
+        uint8_t* const my_stg = stg + (size_t)ew * p.bufs * TL_STG;
+        const uint32_t tempty_u32 = CG2 ? ptx::mapa_u32(ptx::smem_u32(tempty), 0u) : ptx::smem_u32(tempty);
+        int acc = 0, buf = 0;
+        uint32_t acc_ph = 0;
+        // the staging buffer that was handed to TMA longest ago, once it has been read
+        auto buffer = [&]() {
+            if (lane == 0) {
+                if (p.bufs == 2) ptx::tma_store_wait_read<1>(); else ptx::tma_store_wait_read<0>();
+            }
+            __syncwarp();
+            uint8_t* b = my_stg + buf * TL_STG;
+            buf = p.bufs == 2 ? buf ^ 1 : 0;
+            return b;
+        };
+        pdl_wait();
+        for (int i = worker; i < tiles; i += nworkers) {
+            int mt, nt, split, kb0, kb1;
+            item(i, mt, nt, split, kb0, kb1);
+            const int row0 = mt * TM + (int)rank * 128 + lane_group * 32;
+            const uint32_t taddr = tmem_base + ((uint32_t)(lane_group * 32) << 16) + (uint32_t)(acc * p.acc_stride);
+            TlPass<T, KIND, NP> pass;
+            if (KIND != LIN_WEIGHT) pass.request(p, (long long)row0 + lane, nt * p.BN + c_lo);
+            bool ok = true;
+            if (lane == 0) ok = wait_bar(tfull + acc, acc_ph, abort_flag, p.status, 24);  // one poller a warp
+            ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+            if (!ok) break;
+            ptx::tc_fence_after();
+            auto release_acc = [&]() {  // this warp is done reading the tile's accumulators
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (CG2) ptx::mbar_arrive_cluster(tempty_u32 + 8u * (uint32_t)acc); else ptx::mbar_arrive(tempty + acc);
+                }
+            };
+            if (KIND == LIN_WEIGHT) {
+                for (int c = 0; c < ncol; c += 32) {
+                    const int col = nt * p.BN + c_lo + c;
+                    if (col >= p.N) break;
+                    uint32_t r[32];
+                    ptx::tmem_ld_32x32b_x32(taddr + (uint32_t)(c_lo + c), r);
+                    ptx::tmem_ld_wait();
+                    uint8_t* b = buffer();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(b + lane * 128 + ((j ^ (lane & 7)) * 16)) = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+                    ptx::fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        ptx::tma_store_3d(&p.tmOut, b, col, row0, split);
+                        ptx::tma_store_commit();
+                    }
+                    __syncwarp();
+                }
+                if (p.db && team == 0) {
+                    uint32_t r[16];
+                    ptx::tmem_ld_32x32b_x16(taddr + (uint32_t)p.BN, r);
+                    ptx::tmem_ld_wait();
+                    // (a slice without a k-block of this column tile's share has nothing in these columns)
+                    const int firstkb = kb0 + ((nt - kb0 % p.n_tiles) + p.n_tiles) % p.n_tiles;
+                    if (row0 + lane < p.M) p.db[((size_t)split * p.n_tiles + nt) * p.M + row0 + lane] = firstkb < kb1 ? __uint_as_float(r[0]) : 0.f;
+                    __syncwarp();
+                }
+                release_acc();
+            } else {
+                for (int c = 0; c < ncol; c += NP) {
+                    const int col = nt * p.BN + c_lo + c;
+                    const bool last = c + NP >= ncol;
+                    if (c > 0) pass.request(p, (long long)row0 + lane, col);
+                    auto release = [&]() {
+                        if (last) release_acc();
+                    };
+                    if (col >= p.N) {  // wholly behind the last column
+                        release();
+                        continue;
+                    }
+                    pass.finish(p, taddr + (uint32_t)(c_lo + c), lane, row0, col, release, buffer);
+                }
+            }
+            acc ^= 1;
+            if (acc == 0) acc_ph ^= 1u;
+        }
+        // the staging rows must have been read before this CTA's shared memory is released
+        if (lane == 0) ptx::tma_store_wait_read<0>();
+        __syncwarp();
+    }
+    __syncwarp();  // (the cluster barrier and the release of TMEM want whole warps)
+    ptx::tc_fence_before();
+    if (CG2) ptx::cluster_sync_all(); else __syncthreads();  // pairs: neither CTA may leave while the other still uses its memory
+    if (warp == 1) {
+        ptx::tc_fence_after();
+        if (CG2) ptx::tmem_dealloc_cg2(tmem_base, 512); else ptx::tmem_dealloc(tmem_base, 512);
+    }
+}
+
+}  // namespace nbcbs
