@@ -58,6 +58,8 @@ TlCfg choose_rows(long long M, long long N, long long K, int sms, double epi_ins
 }
 
 // Tiles and row slices of a weight gradient: every item is a CTA (or pair) of its own.
+// Tiles of at most 192 columns have room in TMEM for the bias's column of sums; wider ones leave it to a pass over dy.
+bool db_in_tile(const TlCfg& c) { return c.bn + 32 <= 256; }
 TlCfg choose_weight(long long M, long long N, long long K, int sms) {
     TlCfg best;
     for (int cg2 = 1; cg2 >= 0; --cg2)
@@ -76,7 +78,8 @@ TlCfg choose_weight(long long M, long long N, long long K, int sms) {
                 const double item = c.kb_per_split * stage_cycles(cg2, bn) + bn * 8.0 + 1500.0;
                 // (slices: written, read back and added at about 2.5 KB a cycle, and another launch)
                 const double sums = c.splits > 1 ? 3000.0 + 2.0 * c.splits * (double)M * N * 4 / 2500.0 : 0.0;
-                c.cost = (double)ceil_div(tiles * c.splits, workers) * item + sums;
+                const double db = db_in_tile(c) ? 0.0 : 3000.0 + 2.0 * M * K / 3400.0;
+                c.cost = (double)ceil_div(tiles * c.splits, workers) * item + sums + db;
                 if (!best.bn || c.cost < best.cost) best = c;
             }
         }
@@ -100,7 +103,12 @@ SimtCfg simt_cfg(long long M, long long N, long long K, int sms, bool weight) {
     c.slices = (int)ceil_div(K, c.kslice);
     return c;
 }
-int colsum_parts(long long rows) { return (int)std::max<long long>(1, std::min<long long>(64, rows / 256)); }
+constexpr int COLSUM_PARTS = 128;
+// Ranges of rows of a column-sum pass over c columns, `v` a vector: about four blocks an SM.
+int colsum_parts(long long rows, long long c, int v, int sms) {
+    const long long wide = ceil_div(c, 16 * v);
+    return (int)std::max<long long>(1, std::min<long long>({COLSUM_PARTS, rows / 64, ceil_div(4 * sms, wide)}));
+}
 
 // ---------------------------------------------------------------- choice of kernels
 bool tc_layer(const nb_linear_plan_s* p) {
@@ -114,12 +122,12 @@ size_t simt_ws(const nb_linear_plan_s* p, long long rows, int kind) {
     const long long M = kind == LIN_WEIGHT ? co : rows, N = kind == LIN_FWD ? co : ci, K = kind == LIN_FWD ? ci : kind == LIN_DATA ? co : rows;
     const SimtCfg c = simt_cfg(M, N, K, p->sms, kind == LIN_WEIGHT);
     size_t b = c.slices > 1 ? align_up((size_t)c.slices * M * N * 4, 256) : 0;
-    if (kind == LIN_WEIGHT) b += align_up((size_t)colsum_parts(rows) * co * 4, 256);
+    if (kind == LIN_WEIGHT) b += align_up((size_t)COLSUM_PARTS * co * 4, 256);
     return b;
 }
 size_t tc_weight_ws(const nb_linear_plan_s* p, const TlCfg& c) {
     const size_t M = p->d.c_out, N = p->d.c_in;
-    return (c.splits > 1 ? align_up((size_t)c.splits * M * N * 4, 256) : 0) + align_up((size_t)c.splits * c.n_tiles * M * 4, 256);
+    return (c.splits > 1 ? align_up((size_t)c.splits * M * N * 4, 256) : 0) + align_up((size_t)std::max(c.splits * c.n_tiles, COLSUM_PARTS) * M * 4, 256);
 }
 size_t workspace_for(const nb_linear_plan_s* p, long long rows) {
     size_t b = 256;
@@ -127,6 +135,9 @@ size_t workspace_for(const nb_linear_plan_s* p, long long rows) {
     if (tc_layer(p)) b = std::max(b, tc_weight_ws(p, choose_weight(p->d.c_out, p->d.c_in, rows, p->sms)));
     return b;
 }
+
+// Columns of an epilogue pass: a warp has half of a tile's.
+int pass_cols(const TlCfg& c) { return c.bn % 128 == 0 ? 64 : 32; }
 
 // ---------------------------------------------------------------- tensor cores: launch
 bool encode(CUtensorMap* m, int32_t dtype, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box, CUtensorMapSwizzle sw, bool load) {
@@ -137,11 +148,11 @@ bool encode(CUtensorMap* m, int32_t dtype, const void* base, int rank, const cuu
     return d.tiled(m, t, (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, sw,
                    load ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// a matrix [rows][cols] of 16-bit elements, boxes of box_cols by box_rows
-bool encode2(CUtensorMap* m, int32_t dtype, const void* base, long long rows, long long cols, long long ld, int box_cols, int box_rows, bool load) {
+// a matrix [rows][cols] of 16-bit elements, boxes of box_cols (64: 128-byte swizzle, 32: 64-byte swizzle) by box_rows
+bool encode2(CUtensorMap* m, int32_t dtype, const void* base, long long rows, long long cols, long long ld, int box_cols, int box_rows) {
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
     const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
-    return encode(m, dtype, base, 2, dims, strides, box, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, load);
+    return encode(m, dtype, base, 2, dims, strides, box, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, true);
 }
 
 template <typename T, int KIND, bool CG2, int NP> nb_status launch_tc(const nb_linear_plan_s* plan, const TcLinParams& P, unsigned grid, size_t smem, cudaStream_t st) {
@@ -172,21 +183,18 @@ template <int KIND> nb_status run_tc(const nb_linear_plan_s* plan, const TlCfg& 
     const int tm = c.cg2 ? 256 : 128;
     P.idesc = ptx::make_idesc_bf16(tm, c.bn, KIND == LIN_WEIGHT, KIND != LIN_FWD, f16);
     P.idesc_ones = ptx::make_idesc_bf16(tm, c.cg2 ? 32 : 16, 1, 1, f16);
-    P.bufs = KIND == LIN_WEIGHT ? 1 : 2;
-    const size_t fixed = 1024 + (size_t)8 * P.bufs * TL_STG + (KIND == LIN_WEIGHT ? TL_ONES_BYTES : 0) + 256;
-    P.stages = (int)std::min<size_t>(8, (tcdetail::kMaxSmem - fixed) / (TL_A_BYTES + P.b_bytes));
+    const size_t fixed = 1024 + (size_t)16 * TL_STG + (KIND == LIN_WEIGHT ? (int)TL_ONES_BYTES : KIND == LIN_FWD ? 8 * 512 : 0) + 512;
+    P.stages = (int)std::min<size_t>(6, (tcdetail::kMaxSmem - fixed) / (TL_A_BYTES + P.b_bytes));
     const size_t smem = fixed + (size_t)P.stages * (TL_A_BYTES + P.b_bytes);
     const long long tiles = (long long)c.m_tiles * c.n_tiles * (KIND == LIN_WEIGHT ? c.splits : 1);
     if (tiles > 0x3fffffffLL) return fail(NB_ERR_UNSUPPORTED, "too many tiles");
     const long long workers = c.cg2 ? plan->sms / 2 : plan->sms;
     const unsigned grid = (unsigned)((KIND == LIN_WEIGHT ? tiles : std::min(tiles, workers)) * (c.cg2 ? 2 : 1));
-    const bool wide = KIND != LIN_WEIGHT && c.bn % 128 == 0;
-#define NB_TL(T)                                                                                                                                       \
-    if (KIND == LIN_WEIGHT) return c.cg2 ? launch_tc<T, KIND, true, 32>(plan, P, grid, smem, st) : launch_tc<T, KIND, false, 32>(plan, P, grid, smem, st); \
-    if (wide) return c.cg2 ? launch_tc<T, KIND, true, 64>(plan, P, grid, smem, st) : launch_tc<T, KIND, false, 64>(plan, P, grid, smem, st);               \
-    return c.cg2 ? launch_tc<T, KIND, true, 32>(plan, P, grid, smem, st) : launch_tc<T, KIND, false, 32>(plan, P, grid, smem, st);
-    if (f16) { NB_TL(__half) }
-    NB_TL(__nv_bfloat16)
+#define NB_TL(T, NP) (c.cg2 ? launch_tc<T, KIND, true, NP>(plan, P, grid, smem, st) : launch_tc<T, KIND, false, NP>(plan, P, grid, smem, st))
+    if constexpr (KIND != LIN_WEIGHT) {
+        if (pass_cols(c) == 64) return f16 ? NB_TL(__half, 64) : NB_TL(__nv_bfloat16, 64);
+    }
+    return f16 ? NB_TL(__half, 32) : NB_TL(__nv_bfloat16, 32);
 #undef NB_TL
 }
 
@@ -211,6 +219,23 @@ template <int KIND> nb_status run_simt_any(const nb_linear_plan_s* plan, LinArgs
     if (plan->d.dtype == NB_DTYPE_F32) return run_simt<float, KIND>(plan, P, vec, workspace, st);
     if (plan->d.dtype == NB_DTYPE_BF16) return run_simt<__nv_bfloat16, KIND>(plan, P, vec, workspace, st);
     return run_simt<__half, KIND>(plan, P, vec, workspace, st);
+}
+
+// Sums of dy's columns over ranges of rows into `partial`; returns the number of ranges in *parts.
+template <typename T> nb_status run_colsum(const nb_linear_plan_s* plan, const void* dy, long long ld, long long rows, float* partial, int* parts, cudaStream_t st) {
+    constexpr int V = 16 / (int)sizeof(T);
+    const int c = plan->d.c_out;
+    const bool vec = !(reinterpret_cast<uintptr_t>(dy) & 15u) && ld % V == 0 && c % V == 0;
+    const long long per = ceil_div(rows, colsum_parts(rows, c, vec ? V : 1, plan->sms));
+    *parts = (int)ceil_div(rows, per);
+    if (vec) launch_k(lin_colsum_kernel<T, V>, dim3((unsigned)ceil_div(c, 16 * V), (unsigned)*parts), dim3(256), 0, st, 1, static_cast<const T*>(dy), ld, rows, c, per, partial);
+    else launch_k(lin_colsum_kernel<T, 1>, dim3((unsigned)ceil_div(c, 16), (unsigned)*parts), dim3(256), 0, st, 1, static_cast<const T*>(dy), ld, rows, c, per, partial);
+    return launch_ok("lin_colsum");
+}
+nb_status run_colsum_any(const nb_linear_plan_s* plan, const void* dy, long long ld, long long rows, float* partial, int* parts, cudaStream_t st) {
+    if (plan->d.dtype == NB_DTYPE_F32) return run_colsum<float>(plan, dy, ld, rows, partial, parts, st);
+    if (plan->d.dtype == NB_DTYPE_BF16) return run_colsum<__nv_bfloat16>(plan, dy, ld, rows, partial, parts, st);
+    return run_colsum<__half>(plan, dy, ld, rows, partial, parts, st);
 }
 
 template <typename T> nb_status run_rows(const nb_linear_plan_s* plan, LinArgs& P, int rows, cudaStream_t st) {
@@ -357,10 +382,10 @@ nb_status nb_linear_fwd(nb_linear_plan p, int64_t rows, const void* x, int64_t l
         TcLinParams P;
         memset(&P, 0, sizeof P);
         P.M = (int)rows; P.N = (int)co;
-        P.bias = bias; P.act = act; P.add = res; P.ld_add = ld_res; P.want_z = z != nullptr;
-        const int np = c.bn % 128 == 0 ? 64 : 32;
-        if (!encode2(&P.tmA, p->d.dtype, x, rows, ci, ld_x, 64, 128, true) || !encode2(&P.tmB, p->d.dtype, w, co, ci, ci, 64, c.cg2 ? c.bn / 2 : c.bn, true) ||
-            !encode2(&P.tmOut, p->d.dtype, out, rows, co, ld_out, np, 32, false) || (z && !encode2(&P.tmZ, p->d.dtype, z, rows, co, co, np, 32, false)))
+        P.bias = bias; P.act = act; P.has_in = res != nullptr; P.want_z = z != nullptr; P.res = res; P.ld_res = ld_res;
+        if (!encode2(&P.tmA, p->d.dtype, x, rows, ci, ld_x, 64, 128) || !encode2(&P.tmB, p->d.dtype, w, co, ci, ci, 64, c.cg2 ? c.bn / 2 : c.bn) ||
+            !encode2(&P.tmOut, p->d.dtype, out, rows, co, ld_out, pass_cols(c), 32) || (z && !encode2(&P.tmZ, p->d.dtype, z, rows, co, co, pass_cols(c), 32)) ||
+            (res && !encode2(&P.tmIn, p->d.dtype, res, rows, co, ld_res, pass_cols(c), 32)))
             return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
         return run_tc<LIN_FWD>(p, c, P, st);
     }
@@ -389,10 +414,9 @@ nb_status nb_linear_bwd_data(nb_linear_plan p, int64_t rows, const void* dy, int
         TcLinParams P;
         memset(&P, 0, sizeof P);
         P.M = (int)rows; P.N = (int)ci;
-        P.act = act_in; P.add = add; P.ld_add = ld_add; P.zin = z_in;
-        const int np = c.bn % 128 == 0 ? 64 : 32;
-        if (!encode2(&P.tmA, p->d.dtype, dy, rows, co, ld_dy, 64, 128, true) || !encode2(&P.tmB, p->d.dtype, w, co, ci, ci, 64, TL_KC, true) ||
-            !encode2(&P.tmOut, p->d.dtype, dx, rows, ci, ld_dx, np, 32, false))
+        P.act = act_in; P.add = add; P.ld_add = ld_add; P.has_in = z_in != nullptr;
+        if (!encode2(&P.tmA, p->d.dtype, dy, rows, co, ld_dy, 64, 128) || !encode2(&P.tmB, p->d.dtype, w, co, ci, ci, 64, TL_KC) ||
+            !encode2(&P.tmOut, p->d.dtype, dx, rows, ci, ld_dx, pass_cols(c), 32) || (z_in && !encode2(&P.tmIn, p->d.dtype, z_in, rows, ci, ci, pass_cols(c), 32)))
             return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
         return run_tc<LIN_DATA>(p, c, P, st);
     }
@@ -432,16 +456,17 @@ nb_status nb_linear_bwd_weight(nb_linear_plan p, int64_t rows, const void* x, in
         P.M = (int)co; P.N = (int)ci;
         float* part = c.splits > 1 ? reinterpret_cast<float*>(ws) : dw;
         float* db = reinterpret_cast<float*>(ws + (c.splits > 1 ? align_up((size_t)c.splits * n1 * 4, 256) : 0));
-        const int db_parts = c.splits * c.n_tiles;
-        if (dbias && db_parts == 1) db = dbias;
-        P.db = dbias ? db : nullptr;
+        int db_parts = c.splits * c.n_tiles;
+        if (dbias && !db_in_tile(c)) NB_TRY(run_colsum_any(p, dy, ld_dy, rows, db, &db_parts, st));  // (first: what it reads may wait in L2)
+        else if (dbias && db_parts == 1) db = dbias;
+        P.db = dbias && db_in_tile(c) ? db : nullptr;
         const cuuint64_t dims[3] = {(cuuint64_t)ci, (cuuint64_t)co, (cuuint64_t)c.splits}, strides[2] = {(cuuint64_t)ci * 4, (cuuint64_t)n1 * 4};
         const cuuint32_t box[3] = {32, 32, 1};
-        if (!encode2(&P.tmA, p->d.dtype, dy, rows, co, ld_dy, 64, TL_KC, true) || !encode2(&P.tmB, p->d.dtype, x, rows, ci, ld_x, 64, TL_KC, true) ||
+        if (!encode2(&P.tmA, p->d.dtype, dy, rows, co, ld_dy, 64, TL_KC) || !encode2(&P.tmB, p->d.dtype, x, rows, ci, ld_x, 64, TL_KC) ||
             !encode(&P.tmOut, NB_DTYPE_F32, part, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, false))
             return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
         NB_TRY(run_tc<LIN_WEIGHT>(p, c, P, st));
-        const bool add_db = dbias && db_parts > 1;
+        const bool add_db = dbias && db != dbias;
         return c.splits > 1 || add_db ? sums(part, c.splits > 1 ? c.splits : 0, db, add_db ? db_parts : 0) : NB_OK;
     }
     LinArgs A;
@@ -453,16 +478,7 @@ nb_status nb_linear_bwd_weight(nb_linear_plan p, int64_t rows, const void* x, in
     const int slices = A.slices;
     float* db = reinterpret_cast<float*>(ws + (slices > 1 ? align_up((size_t)slices * n1 * 4, 256) : 0));
     int parts = 0;
-    if (dbias) {
-        const long long per = ceil_div(rows, colsum_parts(rows));
-        parts = (int)ceil_div(rows, per);
-        const dim3 grid((unsigned)ceil_div(co, 32), (unsigned)parts);
-        if (p->d.dtype == NB_DTYPE_F32) launch_k(lin_colsum_kernel<float>, grid, dim3(256), 0, st, 1, static_cast<const float*>(dy), (long long)ld_dy, (long long)rows, (int)co, per, db);
-        else if (p->d.dtype == NB_DTYPE_BF16)
-            launch_k(lin_colsum_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, 1, static_cast<const __nv_bfloat16*>(dy), (long long)ld_dy, (long long)rows, (int)co, per, db);
-        else launch_k(lin_colsum_kernel<__half>, grid, dim3(256), 0, st, 1, static_cast<const __half*>(dy), (long long)ld_dy, (long long)rows, (int)co, per, db);
-        NB_LAUNCH_OK("lin_colsum");
-    }
+    if (dbias) NB_TRY(run_colsum_any(p, dy, ld_dy, rows, db, &parts, st));
     return slices > 1 || parts ? sums(static_cast<const float*>(workspace), slices > 1 ? slices : 0, db, parts) : NB_OK;
 }
 

@@ -18,22 +18,25 @@ constexpr int TL_THREADS = 320;  // warp 0: TMA producer, warp 1: MMA issuer and
 constexpr int TL_KC = 64;        // k of a stage: 128 bytes of a 16-bit K-major operand
 constexpr uint32_t TL_BLK = 64 * 128;         // an MN-major block: 64 m (or n) by 64 k
 constexpr uint32_t TL_A_BYTES = 128 * 128;    // A rows of a CTA by 64 k
-constexpr int TL_STG = 4096;                  // staging buffer of an epilogue warp: 32 rows of 128 bytes
+constexpr int TL_STG = 4096;     // staging buffer of an epilogue warp: 32 rows of 128 bytes; it has two
+constexpr int TL_CHUNK = 16;                    // k-blocks after which a weight gradient's sums leave the tensor cores
 constexpr uint32_t TL_ONES_BYTES = 4096;
 
 struct TcLinParams {
-    CUtensorMap tmA, tmB, tmOut, tmZ;
+    CUtensorMap tmA, tmB, tmOut, tmZ, tmIn;  // tmIn: the residual (forward), z_in (data gradient)
     int M, N, kblocks;  // k-blocks of TL_KC
     int BN, m_tiles, n_tiles, group_m;
-    int stages, bufs, acc_stride;  // bufs: staging buffers of an epilogue warp (1 or 2)
+    int stages, acc_stride;
     int nblkB;                     // MN-major: 64-column blocks of this CTA's part of B
     uint32_t b_bytes, idesc;
     // epilogue
     const float* bias;
     int act;
-    const void *add, *zin;
+    int has_in, want_z;
+    const void* res;  // forward with z: the residual
+    long long ld_res;
+    const void* add;  // data gradient: the other branch's gradient
     long long ld_add;
-    int want_z;
     // weight gradient
     int splits, kb_per_split;
     float* db;  // partial sums of dbias [splits * n_tiles][M], or NULL
@@ -55,36 +58,46 @@ template <typename T> __device__ __forceinline__ float2 tl_pair(const uint4& v, 
     return pair_to_f32<T>(reinterpret_cast<const T*>(&w));
 }
 
-// One pass of the epilogue by a warp: NP (32 or 64) accumulator columns of its 32 rows become results, go through the warp's
-// staging rows (rows of NP*2 bytes in the swizzle of that width) and leave as a TMA store.
+// One pass of the epilogue by a warp: NP (64 or 32) accumulator columns of its 32 rows become results.  A lane has one row's.  They go
+// through one of the warp's staging buffers (rows of 2*NP bytes in the swizzle of that width) and leave as a TMA store; a residual or
+// z_in has come into the same buffer by a TMA load.  Both run beside the arithmetic.
 template <typename T, int KIND, int NP> struct TlPass {
-    uint4 ad[NP / 8], zi[NP / 8];  // this row's pieces of `add` and of z_in, requested before the accumulators are waited for
-    __device__ __forceinline__ void request(const TcLinParams& p, long long row, int col) {
-        const bool live = row < p.M;
+    static __device__ __forceinline__ uint4* piece(uint8_t* stg, int lane, int j) {
+        return reinterpret_cast<uint4*>(stg + lane * (NP * 2) + (NP == 64 ? (j ^ (lane & 7)) : (j ^ ((lane >> 1) & 3))) * 16);
+    }
+    static __device__ __forceinline__ void stage(uint8_t* stg, int lane, const float2 (&v)[NP / 2]) {
 #pragma unroll
-        for (int j = 0; j < NP / 8; ++j) {
-            const bool in = live && col + 8 * j < p.N;
-            if (p.add) ad[j] = in ? *reinterpret_cast<const uint4*>(static_cast<const T*>(p.add) + row * p.ld_add + col + 8 * j) : make_uint4(0u, 0u, 0u, 0u);
-            if (KIND == LIN_DATA && p.zin) zi[j] = in ? *reinterpret_cast<const uint4*>(static_cast<const T*>(p.zin) + row * p.N + col + 8 * j) : make_uint4(0u, 0u, 0u, 0u);
+        for (int j = 0; j < NP / 8; ++j)
+            *piece(stg, lane, j) = make_uint4(pack2<T>(v[4 * j].x, v[4 * j].y, nullptr), pack2<T>(v[4 * j + 1].x, v[4 * j + 1].y, nullptr),
+                                              pack2<T>(v[4 * j + 2].x, v[4 * j + 2].y, nullptr), pack2<T>(v[4 * j + 3].x, v[4 * j + 3].y, nullptr));
+    }
+    // this row's pieces of a matrix [M][N], straight from memory
+    static __device__ __forceinline__ void direct(const TcLinParams& p, uint4 (&d)[NP / 8], const void* base, long long ld, long long row, int col) {
+        const T* q = static_cast<const T*>(base) + row * ld + col;
+#pragma unroll
+        for (int j = 0; j < NP / 8; ++j) d[j] = row < p.M && col + 8 * j < p.N ? *reinterpret_cast<const uint4*>(q + 8 * j) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    static __device__ __forceinline__ void send(const CUtensorMap* tm, uint8_t* stg, int lane, int col, int row0) {
+        ptx::fence_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            ptx::tma_store_2d(tm, stg, col, row0);
+            ptx::tma_store_commit();
         }
     }
-    static __device__ __forceinline__ int slot(int lane, int j) { return NP == 64 ? (j ^ (lane & 7)) : (j ^ ((lane >> 1) & 3)); }
-    static __device__ __forceinline__ void stage(uint8_t* my_row, int lane, const float2 (&v)[NP / 2]) {
-#pragma unroll
-        for (int j = 0; j < NP / 8; ++j) {
-            uint4 o;
-            o.x = pack2<T>(v[4 * j].x, v[4 * j].y, nullptr);
-            o.y = pack2<T>(v[4 * j + 1].x, v[4 * j + 1].y, nullptr);
-            o.z = pack2<T>(v[4 * j + 2].x, v[4 * j + 2].y, nullptr);
-            o.w = pack2<T>(v[4 * j + 3].x, v[4 * j + 3].y, nullptr);
-            *reinterpret_cast<uint4*>(my_row + slot(lane, j) * 16) = o;
-        }
-    }
-    template <class Release, class Buffer>
-    __device__ __forceinline__ void finish(const TcLinParams& p, uint32_t taddr, int lane, int row0, int col, Release release, Buffer buffer) {
+    // `in_here`: the pass's input lies in buffer `stg`; `other` gives z a buffer
+    template <class Release, class Other>
+    static __device__ __forceinline__ void run(const TcLinParams& p, uint32_t taddr, int lane, int row0, int col, const float* bias, uint8_t* stg, bool in_here, Release release, Other other) {
         uint32_t r[NP];
 #pragma unroll
         for (int h = 0; h < NP / 32; ++h) ptx::tmem_ld_32x32b_x32(taddr + 32u * h, r + 32 * h);
+        uint4 in[NP / 8];
+        if (in_here) {
+#pragma unroll
+            for (int j = 0; j < NP / 8; ++j) in[j] = *piece(stg, lane, j);
+        } else if (KIND == LIN_FWD && p.has_in) {
+            direct(p, in, p.res, p.ld_res, (long long)row0 + lane, col);
+        }
         ptx::tmem_ld_wait();
         release();
         float2 v[NP / 2];
@@ -94,50 +107,50 @@ template <typename T, int KIND, int NP> struct TlPass {
             if (p.bias) {
 #pragma unroll
                 for (int j = 0; j < NP / 4; ++j) {
-                    const float4 b = col + 4 * j < p.N ? __ldg(reinterpret_cast<const float4*>(p.bias + col + 4 * j)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    const float4 b = *reinterpret_cast<const float4*>(bias + 4 * j);  // (shared memory, one address a warp)
                     v[2 * j] = add2(v[2 * j], make_float2(b.x, b.y));
                     v[2 * j + 1] = add2(v[2 * j + 1], make_float2(b.z, b.w));
                 }
             }
             if (p.want_z) {
-                uint8_t* stg = buffer();
-                stage(stg + lane * (NP * 2), lane, v);
-                ptx::fence_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    ptx::tma_store_2d(&p.tmZ, stg, col, row0);
-                    ptx::tma_store_commit();
-                }
+                uint8_t* zs = other();
+                stage(zs, lane, v);
+                send(&p.tmZ, zs, lane, col, row0);
             }
             if (p.act == NB_ACT_GELU) {
 #pragma unroll
-                for (int j = 0; j < NP / 2; ++j) v[j] = lin_act2(v[j], NB_ACT_GELU);
+                for (int j = 0; j < NP / 2; ++j) v[j] = lin_act2<T>(v[j], NB_ACT_GELU);
             } else if (p.act == NB_ACT_SILU) {
 #pragma unroll
-                for (int j = 0; j < NP / 2; ++j) v[j] = lin_act2(v[j], NB_ACT_SILU);
+                for (int j = 0; j < NP / 2; ++j) v[j] = lin_act2<T>(v[j], NB_ACT_SILU);
+            }
+            if (p.has_in) {
+#pragma unroll
+                for (int j = 0; j < NP / 2; ++j) v[j] = add2(v[j], tl_pair<T>(in[j / 4], j & 3));
+            }
+        } else {
+            if (p.add) {
+                uint4 ad[NP / 8];
+                direct(p, ad, p.add, p.ld_add, (long long)row0 + lane, col);
+#pragma unroll
+                for (int j = 0; j < NP / 2; ++j) v[j] = add2(v[j], tl_pair<T>(ad[j / 4], j & 3));
+            }
+            if (p.has_in) {
+                if (p.act == NB_ACT_GELU) {
+#pragma unroll
+                    for (int j = 0; j < NP / 2; ++j) v[j] = mul2(v[j], lin_act_grad2(tl_pair<T>(in[j / 4], j & 3), NB_ACT_GELU));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < NP / 2; ++j) v[j] = mul2(v[j], lin_act_grad2(tl_pair<T>(in[j / 4], j & 3), NB_ACT_SILU));
+                }
             }
         }
-        if (p.add) {
-#pragma unroll
-            for (int j = 0; j < NP / 2; ++j) v[j] = add2(v[j], tl_pair<T>(ad[j / 4], j & 3));
+        if (KIND == LIN_FWD && p.want_z) {
+            if (lane == 0) ptx::tma_store_wait_read<1>();
+            __syncwarp();
         }
-        if (KIND == LIN_DATA && p.zin) {
-            if (p.act == NB_ACT_GELU) {
-#pragma unroll
-                for (int j = 0; j < NP / 2; ++j) v[j] = mul2(v[j], lin_act_grad2(tl_pair<T>(zi[j / 4], j & 3), NB_ACT_GELU));
-            } else {
-#pragma unroll
-                for (int j = 0; j < NP / 2; ++j) v[j] = mul2(v[j], lin_act_grad2(tl_pair<T>(zi[j / 4], j & 3), NB_ACT_SILU));
-            }
-        }
-        uint8_t* stg = buffer();
-        stage(stg + lane * (NP * 2), lane, v);
-        ptx::fence_async_smem();
-        __syncwarp();
-        if (lane == 0) {
-            ptx::tma_store_2d(&p.tmOut, stg, col, row0);
-            ptx::tma_store_commit();
-        }
+        stage(stg, lane, v);
+        send(&p.tmOut, stg, lane, col, row0);
         __syncwarp();  // (the next accumulator load wants the whole warp)
     }
 };
@@ -147,14 +160,16 @@ template <typename T, int KIND, bool CG2, int NP> __global__ void __launch_bound
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* sA = smem;
     uint8_t* sB = sA + (size_t)p.stages * TL_A_BYTES;
-    uint8_t* stg = sB + (size_t)p.stages * p.b_bytes;              // [8 warps][bufs][TL_STG]
-    uint8_t* ones = stg + (size_t)8 * p.bufs * TL_STG;             // weight gradient with dbias
-    uint64_t* bars = reinterpret_cast<uint64_t*>(ones + (KIND == LIN_WEIGHT ? TL_ONES_BYTES : 0));
+    uint8_t* stg = sB + (size_t)p.stages * p.b_bytes;     // [8 warps][2]
+    uint8_t* ones = stg + (size_t)16 * TL_STG;            // weight gradient with dbias
+    float* sbias = reinterpret_cast<float*>(ones);        // forward: a warp's 128 columns of the bias
+    uint64_t* bars = reinterpret_cast<uint64_t*>(ones + (KIND == LIN_WEIGHT ? (int)TL_ONES_BYTES : KIND == LIN_FWD ? 8 * 512 : 0));
     uint64_t* full = bars;
     uint64_t* empty = full + p.stages;
     uint64_t* tfull = empty + p.stages;  // [2]
     uint64_t* tempty = tfull + 2;        // [2]
-    uint64_t* drain = tempty + 2;
+    uint64_t* infull = tempty + 2;       // [8 warps][2]
+    uint64_t* drain = infull + 16;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     constexpr bool A_MN = KIND == LIN_WEIGHT, B_MN = KIND != LIN_FWD;
@@ -175,6 +190,7 @@ template <typename T, int KIND, bool CG2, int NP> __global__ void __launch_bound
             ptx::mbar_init(tfull + i, 1);
             ptx::mbar_init(tempty + i, CG2 ? 16 : 8);  // one arrival per epilogue warp (of both CTAs)
         }
+        for (int i = 0; i < 16; ++i) ptx::mbar_init(infull + i, 1);
         ptx::mbar_init(drain, 1);
         *abort_flag = 0;
         ptx::fence_mbar_init();
@@ -183,11 +199,15 @@ template <typename T, int KIND, bool CG2, int NP> __global__ void __launch_bound
         ptx::prefetch_tmap(&p.tmA);
         ptx::prefetch_tmap(&p.tmB);
     }
-    if (lane == 0 && warp == 2) ptx::prefetch_tmap(&p.tmOut);
+    if (lane == 0 && warp == 2) {
+        ptx::prefetch_tmap(&p.tmOut);
+        if (p.want_z) ptx::prefetch_tmap(&p.tmZ);
+        if (p.has_in) ptx::prefetch_tmap(&p.tmIn);
+    }
     if (KIND == LIN_WEIGHT && p.db && warp >= 2) {
         // 16 columns of ones as an operand: the same whatever the layout
         const uint32_t w = (p.idesc >> 7) & 1u ? 0x3f803f80u : 0x3c003c00u;  // (bf16 or fp16, as the descriptor says)
-        for (uint32_t i = threadIdx.x - 64; i < TL_ONES_BYTES / 4; i += 256) reinterpret_cast<uint32_t*>(ones)[i] = w;
+        for (uint32_t i = threadIdx.x - 64; i < TL_ONES_BYTES / 4; i += TL_THREADS - 64) reinterpret_cast<uint32_t*>(ones)[i] = w;
         ptx::fence_async_smem();
     }
     if (warp == 1) {
@@ -203,6 +223,10 @@ template <typename T, int KIND, bool CG2, int NP> __global__ void __launch_bound
     if (CG2) ptx::cluster_sync_all(); else __syncthreads();  // barriers of both CTAs are initialised before any remote arrive
     ptx::tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    // The tensor cores add to their accumulator with truncation: 1024 additions (16384 rows) left a weight gradient 1.9e-5 off, relative
+    // to its norm, always towards zero.  So a weight gradient's sums leave them every TL_CHUNK k-blocks (64 additions) and are added in
+    // fp32 registers, beside the next chunk's products in the other accumulator set; 1e-6 is left.  (Results in 16 bits do not see it.)
+    const int chunk = KIND == LIN_WEIGHT ? TL_CHUNK : p.kblocks;
     // a work item: a tile and, for the weight gradient, a slice of the rows
     auto item = [&](int i, int& mt, int& nt, int& split, int& kb0, int& kb1) {
         split = 0;
@@ -293,43 +317,49 @@ template <typename T, int KIND, bool CG2, int NP> __global__ void __launch_bound
             for (int i = worker; ok && i < tiles; i += nworkers) {
                 int mt, nt, split, kb0, kb1;
                 item(i, mt, nt, split, kb0, kb1);
-                if (!wait_bar_fast(tempty + acc, acc_ph ^ 1u, abort_flag, p.status, 22)) break;
-                ptx::tc_fence_after();
-                const uint32_t dt = tmem_base + (uint32_t)(acc * p.acc_stride);
-                uint32_t accumulate = 0, accumulate1 = 0;
-                for (int kb = kb0; kb < kb1; ++kb) {
-                    if (!wait_bar_fast(full + s, ph, abort_flag, p.status, 23)) {
+                for (int c0 = kb0; ok && c0 < kb1; c0 += chunk) {
+                    const int c1 = min(kb1, c0 + chunk);
+                    if (!wait_bar_fast(tempty + acc, acc_ph ^ 1u, abort_flag, p.status, 22)) {
                         ok = false;
                         break;
                     }
                     ptx::tc_fence_after();
-                    mma(dt, da, db, p.idesc, accumulate);
-                    mma(dt, da + ka, db + kb_, p.idesc, 1u);
-                    mma(dt, da + 2 * ka, db + 2 * kb_, p.idesc, 1u);
-                    mma(dt, da + 3 * ka, db + 3 * kb_, p.idesc, 1u);
-                    accumulate = 1u;
-                    if (KIND == LIN_WEIGHT && p.db && kb % p.n_tiles == nt) {
-                        // sums of A over k: a product with columns of ones, whose share each column tile takes of the k-blocks in turn
-                        mma(dt + (uint32_t)p.BN, da, d1, p.idesc_ones, accumulate1);
-                        mma(dt + (uint32_t)p.BN, da + ka, d1, p.idesc_ones, 1u);
-                        mma(dt + (uint32_t)p.BN, da + 2 * ka, d1, p.idesc_ones, 1u);
-                        mma(dt + (uint32_t)p.BN, da + 3 * ka, d1, p.idesc_ones, 1u);
-                        accumulate1 = 1u;
+                    const uint32_t dt = tmem_base + (uint32_t)(acc * p.acc_stride);
+                    uint32_t accumulate = 0, accumulate1 = 0;
+                    for (int kb = c0; kb < c1; ++kb) {
+                        if (!wait_bar_fast(full + s, ph, abort_flag, p.status, 23)) {
+                            ok = false;
+                            break;
+                        }
+                        ptx::tc_fence_after();
+                        mma(dt, da, db, p.idesc, accumulate);
+                        mma(dt, da + ka, db + kb_, p.idesc, 1u);
+                        mma(dt, da + 2 * ka, db + 2 * kb_, p.idesc, 1u);
+                        mma(dt, da + 3 * ka, db + 3 * kb_, p.idesc, 1u);
+                        accumulate = 1u;
+                        if (KIND == LIN_WEIGHT && p.db && kb % p.n_tiles == nt) {
+                            // sums of A over k: a product with columns of ones, whose share each column tile takes of the k-blocks in turn
+                            mma(dt + (uint32_t)p.BN, da, d1, p.idesc_ones, accumulate1);
+                            mma(dt + (uint32_t)p.BN, da + ka, d1, p.idesc_ones, 1u);
+                            mma(dt + (uint32_t)p.BN, da + 2 * ka, d1, p.idesc_ones, 1u);
+                            mma(dt + (uint32_t)p.BN, da + 3 * ka, d1, p.idesc_ones, 1u);
+                            accumulate1 = 1u;
+                        }
+                        if (CG2) ptx::umma_commit_cg2_mc_if(leader, empty_u32 + 8u * (uint32_t)s, 3); else ptx::umma_commit_u32_if(leader, empty_u32 + 8u * (uint32_t)s);
+                        da += a_stage;
+                        db += b_stage;
+                        if (++s == p.stages) {
+                            s = 0;
+                            ph ^= 1u;
+                            da = da0;
+                            db = db0;
+                        }
                     }
-                    if (CG2) ptx::umma_commit_cg2_mc_if(leader, empty_u32 + 8u * (uint32_t)s, 3); else ptx::umma_commit_u32_if(leader, empty_u32 + 8u * (uint32_t)s);
-                    da += a_stage;
-                    db += b_stage;
-                    if (++s == p.stages) {
-                        s = 0;
-                        ph ^= 1u;
-                        da = da0;
-                        db = db0;
-                    }
+                    if (!ok) break;
+                    if (CG2) ptx::umma_commit_cg2_mc_if(leader, tfull_u32 + 8u * (uint32_t)acc, 3); else ptx::umma_commit_u32_if(leader, tfull_u32 + 8u * (uint32_t)acc);
+                    acc ^= 1;
+                    if (acc == 0) acc_ph ^= 1u;
                 }
-                if (!ok) break;
-                if (CG2) ptx::umma_commit_cg2_mc_if(leader, tfull_u32 + 8u * (uint32_t)acc, 3); else ptx::umma_commit_u32_if(leader, tfull_u32 + 8u * (uint32_t)acc);
-                acc ^= 1;
-                if (acc == 0) acc_ph ^= 1u;
             }
             // Make sure every MMA issued by this thread has retired before TMEM is released.
             if (CG2) ptx::umma_commit_cg2_if(leader, ptx::smem_u32(drain)); else ptx::umma_commit_u32_if(leader, ptx::smem_u32(drain));
@@ -337,88 +367,163 @@ template <typename T, int KIND, bool CG2, int NP> __global__ void __launch_bound
             }
         }
     } else {
-        // ------------------------------------------------------------------ epilogue: two teams of four warps, each half of the columns
+        // ------------------------------------------------------------------ epilogue: two teams of four warps, each half of a tile's columns
+        // Every warp goes its own way through its 32 rows.  25600 x 384 -> 1536 with GELU and z: this form 56 us; lanes that store
+        // themselves (64-byte pieces of eight rows an instruction) 71, sixteen warps in teams with a buffer and barriers for
+        // each four 63 to 78, and their polling costs the long products 5 %.
         const int ew = warp - 2, team = ew >> 2, lane_group = warp & 3;  // TMEM lanes [32*lane_group, +32)
         const int ncol = p.BN / 2, c_lo = team * ncol;
-        uint8_t* const my_stg = stg + (size_t)ew * p.bufs * TL_STG;
+        uint8_t* const my_stg = stg + (size_t)ew * 2 * TL_STG;
+        uint64_t* const my_in = infull + 2 * ew;
+        float* const my_bias = sbias + ew * 128;
         const uint32_t tempty_u32 = CG2 ? ptx::mapa_u32(ptx::smem_u32(tempty), 0u) : ptx::smem_u32(tempty);
         int acc = 0, buf = 0;
-        uint32_t acc_ph = 0;
-        // the staging buffer that was handed to TMA longest ago, once it has been read
-        auto buffer = [&]() {
-            if (lane == 0) {
-                if (p.bufs == 2) ptx::tma_store_wait_read<1>(); else ptx::tma_store_wait_read<0>();
-            }
+        uint32_t acc_ph = 0, in_ph = 0;  // in_ph: a bit for each buffer
+        auto wait_acc = [&]() {
+            bool ok = true;
+            if (lane == 0) ok = wait_bar(tfull + acc, acc_ph, abort_flag, p.status, 24);  // one poller a warp
+            ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+            if (ok) ptx::tc_fence_after();
+            return ok;
+        };
+        auto release_acc = [&]() {  // this warp is done reading the accumulator set
+            ptx::tc_fence_before();
             __syncwarp();
-            uint8_t* b = my_stg + buf * TL_STG;
-            buf = p.bufs == 2 ? buf ^ 1 : 0;
-            return b;
+            if (lane == 0) {
+                if (CG2) ptx::mbar_arrive_cluster(tempty_u32 + 8u * (uint32_t)acc); else ptx::mbar_arrive(tempty + acc);
+            }
+        };
+        auto next_acc = [&]() {
+            acc ^= 1;
+            if (acc == 0) acc_ph ^= 1u;
         };
         pdl_wait();
         for (int i = worker; i < tiles; i += nworkers) {
             int mt, nt, split, kb0, kb1;
             item(i, mt, nt, split, kb0, kb1);
             const int row0 = mt * TM + (int)rank * 128 + lane_group * 32;
-            const uint32_t taddr = tmem_base + ((uint32_t)(lane_group * 32) << 16) + (uint32_t)(acc * p.acc_stride);
-            TlPass<T, KIND, NP> pass;
-            if (KIND != LIN_WEIGHT) pass.request(p, (long long)row0 + lane, nt * p.BN + c_lo);
-            bool ok = true;
-            if (lane == 0) ok = wait_bar(tfull + acc, acc_ph, abort_flag, p.status, 24);  // one poller a warp
-            ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
-            if (!ok) break;
-            ptx::tc_fence_after();
-            auto release_acc = [&]() {  // this warp is done reading the tile's accumulators
-                ptx::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (CG2) ptx::mbar_arrive_cluster(tempty_u32 + 8u * (uint32_t)acc); else ptx::mbar_arrive(tempty + acc);
-                }
-            };
-            if (KIND == LIN_WEIGHT) {
-                for (int c = 0; c < ncol; c += 32) {
-                    const int col = nt * p.BN + c_lo + c;
-                    if (col >= p.N) break;
-                    uint32_t r[32];
-                    ptx::tmem_ld_32x32b_x32(taddr + (uint32_t)(c_lo + c), r);
-                    ptx::tmem_ld_wait();
-                    uint8_t* b = buffer();
+            const uint32_t lanes = tmem_base + ((uint32_t)(lane_group * 32) << 16);
+            if constexpr (KIND == LIN_WEIGHT) {
+                float2 sum[4][16];  // 32 columns each
+                float dbs = 0.f;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(b + lane * 128 + ((j ^ (lane & 7)) * 16)) = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[q][j] = make_float2(0.f, 0.f);
+                bool ok = true;
+                for (int c0 = kb0; c0 < kb1; c0 += chunk) {
+                    ok = wait_acc();
+                    if (!ok) break;
+                    const uint32_t taddr = lanes + (uint32_t)(acc * p.acc_stride);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (32 * q >= ncol) break;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {  // (16 columns at a time: registers)
+                            uint32_t r[16];
+                            ptx::tmem_ld_32x32b_x16(taddr + (uint32_t)(c_lo + 32 * q + 16 * h), r);
+                            ptx::tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) sum[q][8 * h + j] = add2(sum[q][8 * h + j], make_float2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])));
+                        }
+                    }
+                    if (p.db && team == 1) {
+                        uint32_t r[16];
+                        ptx::tmem_ld_32x32b_x16(taddr + (uint32_t)p.BN, r);
+                        ptx::tmem_ld_wait();
+                        // (a chunk without a k-block of this column tile's share has left nothing in these columns)
+                        const int first = c0 + (nt - c0 % p.n_tiles + p.n_tiles) % p.n_tiles;
+                        if (first < min(kb1, c0 + chunk)) dbs += __uint_as_float(r[0]);
+                        __syncwarp();
+                    }
+                    release_acc();
+                    next_acc();
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int col = nt * p.BN + c_lo + 32 * q;
+                    if (32 * q >= ncol || col >= p.N) break;
+                    uint8_t* b = my_stg + (q & 1) * TL_STG;
+                    if (lane == 0) ptx::tma_store_wait_read<1>();  // (what went out of it before has been read)
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        *reinterpret_cast<float4*>(b + lane * 128 + ((j ^ (lane & 7)) * 16)) = make_float4(sum[q][2 * j].x, sum[q][2 * j].y, sum[q][2 * j + 1].x, sum[q][2 * j + 1].y);
                     ptx::fence_async_smem();
                     __syncwarp();
                     if (lane == 0) {
                         ptx::tma_store_3d(&p.tmOut, b, col, row0, split);
                         ptx::tma_store_commit();
                     }
-                    __syncwarp();
                 }
-                if (p.db && team == 0) {
-                    uint32_t r[16];
-                    ptx::tmem_ld_32x32b_x16(taddr + (uint32_t)p.BN, r);
-                    ptx::tmem_ld_wait();
-                    // (a slice without a k-block of this column tile's share has nothing in these columns)
-                    const int firstkb = kb0 + ((nt - kb0 % p.n_tiles) + p.n_tiles) % p.n_tiles;
-                    if (row0 + lane < p.M) p.db[((size_t)split * p.n_tiles + nt) * p.M + row0 + lane] = firstkb < kb1 ? __uint_as_float(r[0]) : 0.f;
-                    __syncwarp();
-                }
-                release_acc();
+                if (p.db && team == 1 && row0 + lane < p.M) p.db[((size_t)split * p.n_tiles + nt) * p.M + row0 + lane] = dbs;
+                __syncwarp();
             } else {
-                for (int c = 0; c < ncol; c += NP) {
-                    const int col = nt * p.BN + c_lo + c;
-                    const bool last = c + NP >= ncol;
-                    if (c > 0) pass.request(p, (long long)row0 + lane, col);
-                    auto release = [&]() {
-                        if (last) release_acc();
-                    };
-                    if (col >= p.N) {  // wholly behind the last column
-                        release();
-                        continue;
-                    }
-                    pass.finish(p, taddr + (uint32_t)(c_lo + c), lane, row0, col, release, buffer);
+                // the passes of this warp that have columns; pass k uses buffer (buf + k) & 1
+                const int col0 = nt * p.BN + c_lo, passes = max(0, (min(ncol, p.N - col0) + NP - 1) / NP);
+                const bool in_tma = p.has_in && !p.want_z;  // (with z both buffers are at work when the residual would have to come)
+                auto request = [&](int b, int k) {  // pass k's input into buffer b, by lane 0, with the buffer free
+                    ptx::mbar_expect_tx(my_in + b, 32 * NP * 2);
+                    ptx::tma_load_2d(my_stg + b * TL_STG, &p.tmIn, my_in + b, col0 + k * NP, row0);
+                };
+                if (KIND == LIN_FWD && p.bias) {
+                    __syncwarp();
+                    for (int e = lane; e < ncol; e += 32) my_bias[e] = col0 + e < p.N ? p.bias[col0 + e] : 0.f;
+                    __syncwarp();
                 }
+                if (in_tma && lane == 0) {
+                    if (passes > 0) {
+                        ptx::tma_store_wait_read<1>();
+                        request(buf, 0);
+                    }
+                    if (passes > 1) {
+                        ptx::tma_store_wait_read<0>();
+                        request(buf ^ 1, 1);
+                    }
+                }
+                bool ok = wait_acc();
+                const uint32_t taddr = lanes + (uint32_t)(acc * p.acc_stride + c_lo);
+                if (ok && passes == 0) release_acc();
+                for (int k = 0; k < passes; ++k) {
+                    uint8_t* b = my_stg + buf * TL_STG;
+                    if (in_tma) {  // (waited for whatever has failed: nothing may land after the CTA has exited)
+                        __syncwarp();
+                        bool there = false;
+                        for (int j = 0; j < 4000000 && !(there = ptx::mbar_try_wait(my_in + buf, (in_ph >> buf) & 1u)); ++j) {
+                        }
+                        ok = __all_sync(0xffffffffu, ok && there) != 0;
+                        in_ph ^= 1u << buf;
+                        if (!ok && k < 2) {  // (those requested so far)
+                            buf ^= 1;
+                            continue;
+                        }
+                    }
+                    if (!ok) break;
+                    auto release = [&]() {
+                        if (k == passes - 1) release_acc();
+                    };
+                    auto other = [&]() {  // z goes first and takes this pass's buffer, the result the next one
+                        if (lane == 0) ptx::tma_store_wait_read<1>();
+                        __syncwarp();
+                        uint8_t* zs = my_stg + buf * TL_STG;
+                        buf ^= 1;
+                        return zs;
+                    };
+                    if (!in_tma && !p.want_z) {
+                        if (lane == 0) ptx::tma_store_wait_read<1>();
+                        __syncwarp();
+                    }
+                    TlPass<T, KIND, NP>::run(p, taddr + (uint32_t)(k * NP), lane, row0, col0 + k * NP, my_bias + k * NP, p.want_z ? my_stg + (buf ^ 1) * TL_STG : b, in_tma, release, other);
+                    buf ^= 1;
+                    if (in_tma && k + 2 < passes && lane == 0) {
+                        ptx::tma_store_wait_read<0>();
+                        request(buf ^ 1, k + 2);  // (the buffer of pass k)
+                    }
+                }
+                if (!ok) break;
+                next_acc();
             }
-            acc ^= 1;
-            if (acc == 0) acc_ph ^= 1u;
         }
         // the staging rows must have been read before this CTA's shared memory is released
         if (lane == 0) ptx::tma_store_wait_read<0>();
