@@ -124,9 +124,11 @@ template <typename T, int KIND> __device__ __forceinline__ void lin_store(const 
     static_cast<T*>(P.out)[m * P.ld_out + n] = from_f32<T>(v);
 }
 
-// Bound: FMA issue.  A block of 256 threads has a [64 x 64] tile, a thread [4 x 4] of it; operand tiles of 16 k travel through
-// registers into shared memory as fp32, k-major, double-buffered.  VEC: every operand row is whole vectors of four.
-constexpr int LS_BM = 64, LS_BN = 64, LS_BK = 16, LS_THREADS = 256, LS_PITCH = 68;
+// Bound: FMA issue.  A block of 256 threads has a [TILE x TILE] tile: 128 (a thread [8 x 8]: four 16-byte shared loads for 64 products) where
+// there are enough of them, else 64 ([4 x 4]), with slices of k that put four blocks on an SM.  Operand tiles of 16 k travel
+// through registers into shared memory as fp32, k-major, double-buffered.  VEC: every operand row is whole vectors of four.
+// 1600 x 384 x 384 forward: 43 us with one 64-tile block an SM, 37 with four; 8000 x 1024 x 1024 480 us (35 TFLOP/s; the library product 360).
+constexpr int LS_BK = 16, LS_THREADS = 256;
 
 // Four elements of an operand stored [outer][inner] at (outer, inner..inner+3) as fp32, zeros outside.
 template <typename T, bool VEC> __device__ __forceinline__ float4 ls_load(const T* p, long long ld, long long outer, long long inner, long long outers, long long inners) {
@@ -152,39 +154,50 @@ template <typename T, bool VEC> __device__ __forceinline__ float4 ls_load(const 
     return v;
 }
 
-template <typename T, int KIND, bool VEC> __global__ void __launch_bounds__(LS_THREADS) lin_simt_kernel(LinArgs P) {
+template <typename T, int KIND, bool VEC, int TILE> __global__ void __launch_bounds__(LS_THREADS, TILE == 128 ? 2 : 4) lin_simt_kernel(LinArgs P) {
     pdl_launch_dependents();
     pdl_wait();
-    __shared__ __align__(16) float sA[2][LS_BK][LS_PITCH], sB[2][LS_BK][LS_PITCH];
+    constexpr int G = TILE / 64;  // groups of four rows (columns) that a thread has, 64 apart
+    constexpr int PITCH = TILE + 4;
+    __shared__ __align__(16) float sA[2][LS_BK][PITCH], sB[2][LS_BK][PITCH];
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-    const long long tiles_n = (P.N + LS_BN - 1) / LS_BN;
-    const long long m0 = blockIdx.x / tiles_n * LS_BM, n0 = blockIdx.x % tiles_n * LS_BN;
+    const long long tiles_n = (P.N + TILE - 1) / TILE;
+    const long long m0 = blockIdx.x / tiles_n * TILE, n0 = blockIdx.x % tiles_n * TILE;
     const long long k0 = (long long)blockIdx.z * P.kslice, k1 = k0 + P.kslice < P.K ? k0 + P.kslice : P.K;
     const T* A = static_cast<const T*>(P.a);
     const T* B = static_cast<const T*>(P.b);
     constexpr bool A_K = KIND != LIN_WEIGHT, B_K = KIND == LIN_FWD;  // k is the contiguous index of the operand
-    // [outer][k]: 64 outer x 4 groups of four k; [k][outer]: 16 k x 16 groups of four outer
-    const int ro = tid & 63, rk = (tid >> 6) * 4, co = (tid & 15) * 4, ck = tid >> 4;
-    float4 ra, rb;
+    // an operand tile is 16 k x TILE outer: stored [outer][k] a thread takes 4 k of G.. of one outer index, stored [k][outer] 4 outer of G k
+    const int ro = tid % TILE, rk = tid / TILE * (4 * G), co = tid % (TILE / 4) * 4, ck = tid / (TILE / 4);
+    constexpr int CK = LS_THREADS / (TILE / 4);  // k between a thread's groups in the second case
+    float4 ra[G], rb[G];
     auto fetch = [&](long long k) {
-        ra = A_K ? ls_load<T, VEC>(A, P.lda, m0 + ro, k + rk, P.M, k1) : ls_load<T, VEC>(A, P.lda, k + ck, m0 + co, k1, P.M);
-        rb = B_K ? ls_load<T, VEC>(B, P.ldb, n0 + ro, k + rk, P.N, k1) : ls_load<T, VEC>(B, P.ldb, k + ck, n0 + co, k1, P.N);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            ra[g] = A_K ? ls_load<T, VEC>(A, P.lda, m0 + ro, k + rk + 4 * g, P.M, k1) : ls_load<T, VEC>(A, P.lda, k + ck + CK * g, m0 + co, k1, P.M);
+            rb[g] = B_K ? ls_load<T, VEC>(B, P.ldb, n0 + ro, k + rk + 4 * g, P.N, k1) : ls_load<T, VEC>(B, P.ldb, k + ck + CK * g, n0 + co, k1, P.N);
+        }
     };
     auto put = [&](int s) {
-        if (A_K) {
-            sA[s][rk][ro] = ra.x; sA[s][rk + 1][ro] = ra.y; sA[s][rk + 2][ro] = ra.z; sA[s][rk + 3][ro] = ra.w;
-        } else {
-            *reinterpret_cast<float4*>(&sA[s][ck][co]) = ra;
-        }
-        if (B_K) {
-            sB[s][rk][ro] = rb.x; sB[s][rk + 1][ro] = rb.y; sB[s][rk + 2][ro] = rb.z; sB[s][rk + 3][ro] = rb.w;
-        } else {
-            *reinterpret_cast<float4*>(&sB[s][ck][co]) = rb;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            if (A_K) {
+                sA[s][rk + 4 * g][ro] = ra[g].x; sA[s][rk + 4 * g + 1][ro] = ra[g].y; sA[s][rk + 4 * g + 2][ro] = ra[g].z; sA[s][rk + 4 * g + 3][ro] = ra[g].w;
+            } else {
+                *reinterpret_cast<float4*>(&sA[s][ck + CK * g][co]) = ra[g];
+            }
+            if (B_K) {
+                sB[s][rk + 4 * g][ro] = rb[g].x; sB[s][rk + 4 * g + 1][ro] = rb[g].y; sB[s][rk + 4 * g + 2][ro] = rb[g].z; sB[s][rk + 4 * g + 3][ro] = rb[g].w;
+            } else {
+                *reinterpret_cast<float4*>(&sB[s][ck + CK * g][co]) = rb[g];
+            }
         }
     };
-    float2 acc[4][2];
+    float2 acc[4 * G][2 * G];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = make_float2(0.f, 0.f);
+    for (int i = 0; i < 4 * G; ++i)
+#pragma unroll
+        for (int j = 0; j < 2 * G; ++j) acc[i][j] = make_float2(0.f, 0.f);
     fetch(k0);
     put(0);
     __syncthreads();
@@ -194,14 +207,19 @@ template <typename T, int KIND, bool VEC> __global__ void __launch_bounds__(LS_T
         if (more) fetch(k + LS_BK);
 #pragma unroll
         for (int kk = 0; kk < LS_BK; ++kk) {
-            const float4 a = *reinterpret_cast<const float4*>(&sA[s][kk][ty * 4]), b = *reinterpret_cast<const float4*>(&sB[s][kk][tx * 4]);
-            const float2 b0 = make_float2(b.x, b.y), b1 = make_float2(b.z, b.w);
-            const float av[4] = {a.x, a.y, a.z, a.w};
+            float av[4 * G];
+            float2 bv[2 * G];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                acc[i][0] = fma2(splat2(av[i]), b0, acc[i][0]);
-                acc[i][1] = fma2(splat2(av[i]), b1, acc[i][1]);
+            for (int g = 0; g < G; ++g) {
+                const float4 a = *reinterpret_cast<const float4*>(&sA[s][kk][64 * g + ty * 4]), b = *reinterpret_cast<const float4*>(&sB[s][kk][64 * g + tx * 4]);
+                av[4 * g] = a.x; av[4 * g + 1] = a.y; av[4 * g + 2] = a.z; av[4 * g + 3] = a.w;
+                bv[2 * g] = make_float2(b.x, b.y);
+                bv[2 * g + 1] = make_float2(b.z, b.w);
             }
+#pragma unroll
+            for (int i = 0; i < 4 * G; ++i)
+#pragma unroll
+                for (int j = 0; j < 2 * G; ++j) acc[i][j] = fma2(splat2(av[i]), bv[j], acc[i][j]);
         }
         if (more) {
             s ^= 1;
@@ -210,16 +228,16 @@ template <typename T, int KIND, bool VEC> __global__ void __launch_bounds__(LS_T
         }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const long long m = m0 + ty * 4 + i;
-        if (m >= P.M) break;
-        const float v[4] = {acc[i][0].x, acc[i][0].y, acc[i][1].x, acc[i][1].y};
+    for (int i = 0; i < 4 * G; ++i) {
+        const long long m = m0 + 64 * (i / 4) + ty * 4 + i % 4;
+        if (m >= P.M) continue;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const long long n = n0 + tx * 4 + j;
-            if (n >= P.N) break;
-            if (P.slices > 1) P.partial[((long long)blockIdx.z * P.M + m) * P.N + n] = v[j];
-            else lin_store<T, KIND>(P, m, n, v[j]);
+        for (int j = 0; j < 4 * G; ++j) {
+            const long long n = n0 + 64 * (j / 4) + tx * 4 + j % 4;
+            if (n >= P.N) continue;
+            const float v = j & 1 ? acc[i][j / 2].y : acc[i][j / 2].x;
+            if (P.slices > 1) P.partial[((long long)blockIdx.z * P.M + m) * P.N + n] = v;
+            else lin_store<T, KIND>(P, m, n, v);
         }
     }
 }
@@ -369,6 +387,62 @@ template <typename T, int R> __global__ void __launch_bounds__(LR_THREADS) lin_r
         float s = 0.f;
         for (int p = 0; p < wpc; ++p) s += red[c * wpc + p][r];
         if (nn < P.N) lin_store<T, LIN_FWD>(P, r, nn, s);
+    }
+}
+
+// ------------------------------------------------------------------------------------------ odd channel counts on the tensor cores
+// TMA wants rows of whole 16-byte vectors: operands of layers with other channel counts are copied into rows padded with zeros, and
+// results out of such rows.  Eight elements of a padded row a thread; 16-bit elements as they are.
+static __global__ void __launch_bounds__(256) lin_pad_kernel(const uint16_t* __restrict__ src, long long ld, long long rows, int cols, int cols8, uint16_t* __restrict__ dst) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int nv = cols8 / 8;
+    const long long n = rows * nv, step = (long long)gridDim.x * 256;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
+        const long long r = i / nv;
+        const int c = (int)(i - r * nv) * 8;
+        const uint16_t* s = src + r * ld + c;
+        uint16_t e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = c + j < cols ? s[j] : (uint16_t)0;
+        uint4 v;
+        v.x = e[0] | (uint32_t)e[1] << 16;
+        v.y = e[2] | (uint32_t)e[3] << 16;
+        v.z = e[4] | (uint32_t)e[5] << 16;
+        v.w = e[6] | (uint32_t)e[7] << 16;
+        *reinterpret_cast<uint4*>(dst + i * 8) = v;
+    }
+}
+static __global__ void __launch_bounds__(256) lin_unpad_kernel(const uint16_t* __restrict__ src, int cols8, long long rows, int cols, uint16_t* __restrict__ dst, long long ld) {
+    pdl_launch_dependents();
+    pdl_wait();
+    // a warp a row at a time: consecutive lanes, consecutive elements
+    const long long warps = (long long)gridDim.x * 8;
+    const int lane = threadIdx.x & 31;
+    for (long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += warps) {
+        const uint16_t* s = src + r * cols8;
+        uint16_t* d = dst + r * ld;
+        int c = lane;
+        for (; c + 96 < cols; c += 128) {
+            const uint16_t a = s[c], b = s[c + 32], e = s[c + 64], f = s[c + 96];
+            d[c] = a;
+            d[c + 32] = b;
+            d[c + 64] = e;
+            d[c + 96] = f;
+        }
+        for (; c < cols; c += 32) d[c] = s[c];
+    }
+}
+// dw [co][ci] from `slices` matrices [co][ci8], in fp64 and their order.
+static __global__ void __launch_bounds__(256) lin_weight_unpad_kernel(const float* __restrict__ part, int slices, long long co, int ci, int ci8, float* __restrict__ dw) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const long long n = co * ci, step = (long long)gridDim.x * 256, one = co * ci8;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
+        const long long r = i / ci, at = r * ci8 + (i - r * ci);
+        double s = 0.0;
+        for (int z = 0; z < slices; ++z) s += (double)part[z * one + at];
+        dw[i] = (float)s;
     }
 }
 

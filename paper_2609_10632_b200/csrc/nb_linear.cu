@@ -88,16 +88,22 @@ TlCfg choose_weight(long long M, long long N, long long K, int sms) {
 
 // ---------------------------------------------------------------- CUDA cores: slices of k
 struct SimtCfg {
+    int tile = 64;
     long long tiles = 0, kslice = 0;
     int slices = 1;
 };
 SimtCfg simt_cfg(long long M, long long N, long long K, int sms, bool weight) {
     SimtCfg c;
-    c.tiles = ceil_div(M, LS_BM) * ceil_div(N, LS_BN);
-    // as many slices as fill the GPU, of 128 products or more each; sums over rows also in slices of at most 4096, which bounds the
-    // rounding errors of an fp32 sum
-    long long s = c.tiles >= sms ? 1 : std::min<long long>(ceil_div(2 * sms, c.tiles), std::max<long long>(1, K / 128));
-    if (weight) s = std::max(s, ceil_div(K, 4096));
+    c.tiles = ceil_div(M, 128) * ceil_div(N, 128);
+    long long s = 1;
+    if (2 * c.tiles >= 3 * sms) {
+        c.tile = 128;
+    } else {
+        c.tiles = ceil_div(M, 64) * ceil_div(N, 64);
+        // as many slices as give an SM four blocks, of 64 products or more each
+        if (c.tiles < 4 * sms) s = std::min<long long>(ceil_div(4 * sms, c.tiles), std::max<long long>(1, K / 64));
+    }
+    if (weight) s = std::max(s, ceil_div(K, 4096));  // which bounds the rounding errors of an fp32 sum over rows
     s = std::min<long long>(s, 1024);
     c.kslice = ceil_div(ceil_div(K, s), LS_BK) * LS_BK;
     c.slices = (int)ceil_div(K, c.kslice);
@@ -114,6 +120,13 @@ int colsum_parts(long long rows, long long c, int v, int sms) {
 bool tc_layer(const nb_linear_plan_s* p) {
     return p->d.dtype != NB_DTYPE_F32 && !(p->d.flags & NB_LINEAR_FLAG_FORCE_SIMT) && p->d.c_in % 8 == 0 && p->d.c_out % 8 == 0;
 }
+// Layers whose channel counts are not multiples of 8 run on padded copies of their operands (bandwidth against the tensor cores' rate);
+// below this many products the copies and launches take longer than the CUDA cores.
+int round8(int c) { return (c + 7) / 8 * 8; }
+bool tc_padded(const nb_linear_plan_s* p, long long rows) {
+    return p->d.dtype != NB_DTYPE_F32 && !(p->d.flags & NB_LINEAR_FLAG_FORCE_SIMT) && (p->d.c_in % 8 || p->d.c_out % 8) &&
+           (double)rows * p->d.c_in * p->d.c_out >= 134217728.0;
+}
 bool few_rows(const nb_linear_plan_s* p, long long rows) { return rows <= 8 && ((size_t)p->d.c_in * size_of(p->d.dtype)) % 16 == 0; }
 bool whole16(const void* q, long long ld, size_t es) { return !(reinterpret_cast<uintptr_t>(q) & 15u) && ((size_t)ld * es) % 16 == 0; }
 
@@ -129,10 +142,19 @@ size_t tc_weight_ws(const nb_linear_plan_s* p, const TlCfg& c) {
     const size_t M = p->d.c_out, N = p->d.c_in;
     return (c.splits > 1 ? align_up((size_t)c.splits * M * N * 4, 256) : 0) + align_up((size_t)std::max(c.splits * c.n_tiles, COLSUM_PARTS) * M * 4, 256);
 }
+size_t rows_bytes(long long rows, int cols) { return align_up((size_t)rows * round8(cols) * 2, 256); }
+size_t padded_ws(const nb_linear_plan_s* p, long long rows) {
+    const int ci = p->d.c_in, co = p->d.c_out;
+    const size_t a = rows_bytes(rows, ci), b = rows_bytes(rows, co), w = rows_bytes(co, ci);
+    const TlCfg c = choose_weight(co, round8(ci), rows, p->sms);
+    const size_t part = align_up((size_t)c.splits * co * round8(ci) * 4, 256) + align_up((size_t)std::max(c.splits * c.n_tiles, COLSUM_PARTS) * co * 4, 256);
+    return std::max({w + a + 3 * b, w + b + 3 * a, a + b + part});  // forward: x; out, z, res.  data: dy; dx, z_in, add.  weight
+}
 size_t workspace_for(const nb_linear_plan_s* p, long long rows) {
     size_t b = 256;
     for (int kind = 0; kind < 3; ++kind) b = std::max(b, simt_ws(p, rows, kind));
     if (tc_layer(p)) b = std::max(b, tc_weight_ws(p, choose_weight(p->d.c_out, p->d.c_in, rows, p->sms)));
+    if (tc_padded(p, rows)) b = std::max(b, padded_ws(p, rows));
     return b;
 }
 
@@ -206,8 +228,13 @@ template <typename T, int KIND> nb_status run_simt(const nb_linear_plan_s* plan,
     P.slices = c.slices;
     P.partial = static_cast<float*>(workspace);
     const dim3 grid((unsigned)c.tiles, 1, (unsigned)c.slices);
-    if (vec) launch_k(lin_simt_kernel<T, KIND, true>, grid, dim3(LS_THREADS), 0, st, 1, P);
-    else launch_k(lin_simt_kernel<T, KIND, false>, grid, dim3(LS_THREADS), 0, st, 1, P);
+    if (c.tile == 128) {
+        if (vec) launch_k(lin_simt_kernel<T, KIND, true, 128>, grid, dim3(LS_THREADS), 0, st, 1, P);
+        else launch_k(lin_simt_kernel<T, KIND, false, 128>, grid, dim3(LS_THREADS), 0, st, 1, P);
+    } else {
+        if (vec) launch_k(lin_simt_kernel<T, KIND, true, 64>, grid, dim3(LS_THREADS), 0, st, 1, P);
+        else launch_k(lin_simt_kernel<T, KIND, false, 64>, grid, dim3(LS_THREADS), 0, st, 1, P);
+    }
     NB_LAUNCH_OK("lin_simt");
     if (KIND != LIN_WEIGHT && c.slices > 1) {
         launch_k(lin_slices_kernel<T, KIND>, dim3((unsigned)std::min<long long>(ceil_div(P.M * P.N, 256), plan->sms * 8)), dim3(256), 0, st, 1, P);
@@ -250,6 +277,63 @@ template <typename T> nb_status run_rows(const nb_linear_plan_s* plan, LinArgs& 
     else launch_k(lin_rows_kernel<T, 8>, dim3(grid), dim3(LR_THREADS), 0, st, 1, P, rows, wpc);
     return launch_ok("lin_rows");
 }
+
+// ---------------------------------------------------------------- tensor cores: the forward product and the data gradient
+// on operands whose rows are whole vectors; N and K may be padded counts (w has c_out rows all the same)
+nb_status tc_fwd(const nb_linear_plan_s* p, long long rows, const void* x, long long ld_x, const void* w, const float* bias, int act, const void* res, long long ld_res, void* z,
+                 void* out, long long ld_out, int ci, int co, cudaStream_t st) {
+    const TlCfg c = choose_rows(rows, co, ci, p->sms, 6.0 + (act ? 10.0 : 0.0) + (z ? 3.0 : 0.0) + (res ? 3.0 : 0.0));
+    TcLinParams P;
+    memset(&P, 0, sizeof P);
+    P.M = (int)rows; P.N = co; P.n_bias = p->d.c_out;
+    P.bias = bias; P.act = act; P.has_in = res != nullptr; P.want_z = z != nullptr; P.res = res; P.ld_res = ld_res;
+    const int np = pass_cols(c);
+    if (!encode2(&P.tmA, p->d.dtype, x, rows, ci, ld_x, 64, 128) || !encode2(&P.tmB, p->d.dtype, w, p->d.c_out, ci, ci, 64, c.cg2 ? c.bn / 2 : c.bn) ||
+        !encode2(&P.tmOut, p->d.dtype, out, rows, co, ld_out, np, 32) || (z && !encode2(&P.tmZ, p->d.dtype, z, rows, co, co, np, 32)) ||
+        (res && !encode2(&P.tmIn, p->d.dtype, res, rows, co, ld_res, np, 32)))
+        return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+    return run_tc<LIN_FWD>(p, c, P, st);
+}
+nb_status tc_data(const nb_linear_plan_s* p, long long rows, const void* dy, long long ld_dy, const void* w, const void* z_in, int act_in, const void* add, long long ld_add, void* dx,
+                  long long ld_dx, int ci, int co, cudaStream_t st) {
+    const TlCfg c = choose_rows(rows, ci, co, p->sms, 6.0 + (z_in ? 16.0 : 0.0) + (add ? 3.0 : 0.0));
+    TcLinParams P;
+    memset(&P, 0, sizeof P);
+    P.M = (int)rows; P.N = ci;
+    P.act = act_in; P.add = add; P.ld_add = ld_add; P.has_in = z_in != nullptr;
+    const int np = pass_cols(c);
+    if (!encode2(&P.tmA, p->d.dtype, dy, rows, co, ld_dy, 64, 128) || !encode2(&P.tmB, p->d.dtype, w, co, ci, ci, 64, TL_KC) ||
+        !encode2(&P.tmOut, p->d.dtype, dx, rows, ci, ld_dx, np, 32) || (z_in && !encode2(&P.tmIn, p->d.dtype, z_in, rows, ci, ci, np, 32)))
+        return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+    return run_tc<LIN_DATA>(p, c, P, st);
+}
+
+// Padded copies in the workspace, one behind the other.
+struct Padded {
+    const nb_linear_plan_s* p;
+    uint8_t* at;
+    cudaStream_t stream;
+    nb_status st = NB_OK;
+    Padded(const nb_linear_plan_s* plan, long long, void* workspace, cudaStream_t s) : p(plan), at(static_cast<uint8_t*>(workspace)), stream(s) {}
+    void* take(long long rows, int cols) {
+        void* d = at;
+        at += rows_bytes(rows, cols);
+        return d;
+    }
+    const void* in(const void* src, long long ld, long long rows, int cols) {
+        void* d = take(rows, cols);
+        const long long n = rows * (round8(cols) / 8);
+        launch_k(lin_pad_kernel, dim3((unsigned)std::min<long long>(ceil_div(n, 256), p->sms * 16)), dim3(256), 0, stream, 1, static_cast<const uint16_t*>(src), ld, rows, cols, round8(cols),
+                 static_cast<uint16_t*>(d));
+        if (st == NB_OK) st = launch_ok("lin_pad");
+        return d;
+    }
+    nb_status out(const void* src, long long rows, int cols, void* dst, long long ld) {
+        launch_k(lin_unpad_kernel, dim3((unsigned)std::min<long long>(ceil_div(rows, 8), p->sms * 16)), dim3(256), 0, stream, 1, static_cast<const uint16_t*>(src), round8(cols), rows, cols,
+                 static_cast<uint16_t*>(dst), ld);
+        return launch_ok("lin_unpad");
+    }
+};
 
 nb_status check_call(const nb_linear_plan_s* plan, int64_t rows) {
     if (!plan) return fail(NB_ERR_INVALID_ARG, "plan is NULL");
@@ -328,7 +412,7 @@ nb_status nb_linear_paths(nb_linear_plan p, int64_t rows, int32_t* paths3) {
     g_err.clear();
     NB_TRY(check_call(p, rows));
     if (!paths3) return fail(NB_ERR_INVALID_ARG, "paths3 is NULL");
-    const int tc = tc_layer(p) ? 1 : 0;
+    const int tc = tc_layer(p) || tc_padded(p, rows) ? 1 : 0;
     paths3[0] = few_rows(p, rows) ? 2 : tc;
     paths3[1] = paths3[2] = tc;
     return NB_OK;
@@ -377,17 +461,19 @@ nb_status nb_linear_fwd(nb_linear_plan p, int64_t rows, const void* x, int64_t l
         if (p->d.dtype == NB_DTYPE_BF16) return run_rows<__nv_bfloat16>(p, A, (int)rows, st);
         return run_rows<__half>(p, A, (int)rows, st);
     }
-    if (tc_layer(p) && whole16(x, ld_x, es) && whole16(out, ld_out, es) && (!res || whole16(res, ld_res, es)) && whole16(z, co, es)) {
-        const TlCfg c = choose_rows(rows, co, ci, p->sms, 6.0 + (act ? 10.0 : 0.0) + (z ? 3.0 : 0.0) + (res ? 3.0 : 0.0));
-        TcLinParams P;
-        memset(&P, 0, sizeof P);
-        P.M = (int)rows; P.N = (int)co;
-        P.bias = bias; P.act = act; P.has_in = res != nullptr; P.want_z = z != nullptr; P.res = res; P.ld_res = ld_res;
-        if (!encode2(&P.tmA, p->d.dtype, x, rows, ci, ld_x, 64, 128) || !encode2(&P.tmB, p->d.dtype, w, co, ci, ci, 64, c.cg2 ? c.bn / 2 : c.bn) ||
-            !encode2(&P.tmOut, p->d.dtype, out, rows, co, ld_out, pass_cols(c), 32) || (z && !encode2(&P.tmZ, p->d.dtype, z, rows, co, co, pass_cols(c), 32)) ||
-            (res && !encode2(&P.tmIn, p->d.dtype, res, rows, co, ld_res, pass_cols(c), 32)))
-            return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
-        return run_tc<LIN_FWD>(p, c, P, st);
+    if (tc_layer(p) && whole16(x, ld_x, es) && whole16(out, ld_out, es) && (!res || whole16(res, ld_res, es)) && whole16(z, co, es))
+        return tc_fwd(p, rows, x, ld_x, w, bias, act, res, ld_res, z, out, ld_out, (int)ci, (int)co, st);
+    if (tc_padded(p, rows)) {
+        Padded S(p, rows, workspace, st);
+        const int ci8 = round8((int)ci), co8 = round8((int)co);
+        const void* xs = S.in(x, ld_x, rows, (int)ci);
+        const void* wp = S.in(w, ci, co, (int)ci);
+        const void* rs = res ? S.in(res, ld_res, rows, (int)co) : nullptr;
+        void *os = S.take(rows, (int)co), *zs = z ? S.take(rows, (int)co) : nullptr;
+        NB_TRY(S.st);
+        NB_TRY(tc_fwd(p, rows, xs, ci8, wp, bias, act, rs, co8, zs, os, co8, ci8, co8, st));
+        if (z) NB_TRY(S.out(zs, rows, (int)co, z, co));
+        return S.out(os, rows, (int)co, out, ld_out);
     }
     return run_simt_any<LIN_FWD>(p, A, vec4(x, ld_x, ci, es) && vec4(w, ci, ci, es), workspace, st);
 }
@@ -409,16 +495,19 @@ nb_status nb_linear_bwd_data(nb_linear_plan p, int64_t rows, const void* dy, int
     NB_TRY(check_ws(workspace, workspace_bytes, workspace_for(p, rows)));
     DeviceGuard on_device(p->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (tc_layer(p) && whole16(dy, ld_dy, es) && whole16(dx, ld_dx, es) && (!add || whole16(add, ld_add, es)) && whole16(z_in, ci, es)) {
-        const TlCfg c = choose_rows(rows, ci, co, p->sms, 6.0 + (z_in ? 16.0 : 0.0) + (add ? 3.0 : 0.0));
-        TcLinParams P;
-        memset(&P, 0, sizeof P);
-        P.M = (int)rows; P.N = (int)ci;
-        P.act = act_in; P.add = add; P.ld_add = ld_add; P.has_in = z_in != nullptr;
-        if (!encode2(&P.tmA, p->d.dtype, dy, rows, co, ld_dy, 64, 128) || !encode2(&P.tmB, p->d.dtype, w, co, ci, ci, 64, TL_KC) ||
-            !encode2(&P.tmOut, p->d.dtype, dx, rows, ci, ld_dx, pass_cols(c), 32) || (z_in && !encode2(&P.tmIn, p->d.dtype, z_in, rows, ci, ci, pass_cols(c), 32)))
-            return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
-        return run_tc<LIN_DATA>(p, c, P, st);
+    if (tc_layer(p) && whole16(dy, ld_dy, es) && whole16(dx, ld_dx, es) && (!add || whole16(add, ld_add, es)) && whole16(z_in, ci, es))
+        return tc_data(p, rows, dy, ld_dy, w, z_in, act_in, add, ld_add, dx, ld_dx, (int)ci, (int)co, st);
+    if (tc_padded(p, rows)) {
+        Padded S(p, rows, workspace, st);
+        const int ci8 = round8((int)ci), co8 = round8((int)co);
+        const void* ds = S.in(dy, ld_dy, rows, (int)co);
+        const void* wp = S.in(w, ci, co, (int)ci);
+        const void* zs = z_in ? S.in(z_in, ci, rows, (int)ci) : nullptr;
+        const void* as = add ? S.in(add, ld_add, rows, (int)ci) : nullptr;
+        void* xs = S.take(rows, (int)ci);
+        NB_TRY(S.st);
+        NB_TRY(tc_data(p, rows, ds, co8, wp, zs, act_in, as, ci8, xs, ci8, ci8, (int)co, st));
+        return S.out(xs, rows, (int)ci, dx, ld_dx);
     }
     LinArgs A;
     memset(&A, 0, sizeof A);
@@ -449,24 +538,44 @@ nb_status nb_linear_bwd_weight(nb_linear_plan p, int64_t rows, const void* x, in
         launch_k(lin_weight_sums_kernel, dim3((unsigned)std::min<long long>(ceil_div(work, 256), p->sms * 8)), dim3(256), 0, st, 1, p1, s1, n1, dw, p2, s2, (int)co, dbias);
         return launch_ok("lin_weight_sums");
     };
-    if (tc_layer(p) && whole16(x, ld_x, es) && whole16(dy, ld_dy, es)) {
-        const TlCfg c = choose_weight(co, ci, rows, p->sms);
+    const bool whole = tc_layer(p) && whole16(x, ld_x, es) && whole16(dy, ld_dy, es), padded = !whole && tc_padded(p, rows);
+    if (whole || padded) {
+        Padded S(p, rows, workspace, st);
+        const int ci8 = round8((int)ci);
+        const void *xs = x, *ds = dy;
+        int64_t lx = ld_x, ld = ld_dy;
+        if (padded) {
+            xs = S.in(x, ld_x, rows, (int)ci);
+            ds = S.in(dy, ld_dy, rows, (int)co);
+            NB_TRY(S.st);
+            lx = ci8;
+            ld = round8((int)co);
+        }
+        const TlCfg c = choose_weight(co, ci8, rows, p->sms);
         TcLinParams P;
         memset(&P, 0, sizeof P);
-        P.M = (int)co; P.N = (int)ci;
-        float* part = c.splits > 1 ? reinterpret_cast<float*>(ws) : dw;
-        float* db = reinterpret_cast<float*>(ws + (c.splits > 1 ? align_up((size_t)c.splits * n1 * 4, 256) : 0));
+        P.M = (int)co; P.N = ci8;
+        const bool sliced = c.splits > 1 || padded;
+        const size_t one = (size_t)co * ci8;
+        float* part = sliced ? reinterpret_cast<float*>(S.at) : dw;
+        float* db = reinterpret_cast<float*>(S.at + (sliced ? align_up(c.splits * one * 4, 256) : 0));
         int db_parts = c.splits * c.n_tiles;
-        if (dbias && !db_in_tile(c)) NB_TRY(run_colsum_any(p, dy, ld_dy, rows, db, &db_parts, st));  // (first: what it reads may wait in L2)
+        if (dbias && !db_in_tile(c)) NB_TRY(run_colsum_any(p, ds, ld, rows, db, &db_parts, st));  // (first: what it reads may wait in L2)
         else if (dbias && db_parts == 1) db = dbias;
         P.db = dbias && db_in_tile(c) ? db : nullptr;
-        const cuuint64_t dims[3] = {(cuuint64_t)ci, (cuuint64_t)co, (cuuint64_t)c.splits}, strides[2] = {(cuuint64_t)ci * 4, (cuuint64_t)n1 * 4};
+        const cuuint64_t dims[3] = {(cuuint64_t)ci8, (cuuint64_t)co, (cuuint64_t)c.splits}, strides[2] = {(cuuint64_t)ci8 * 4, (cuuint64_t)one * 4};
         const cuuint32_t box[3] = {32, 32, 1};
-        if (!encode2(&P.tmA, p->d.dtype, dy, rows, co, ld_dy, 64, TL_KC) || !encode2(&P.tmB, p->d.dtype, x, rows, ci, ld_x, 64, TL_KC) ||
+        if (!encode2(&P.tmA, p->d.dtype, ds, rows, padded ? ld : co, ld, 64, TL_KC) || !encode2(&P.tmB, p->d.dtype, xs, rows, ci8, lx, 64, TL_KC) ||
             !encode(&P.tmOut, NB_DTYPE_F32, part, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, false))
             return fail(NB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
         NB_TRY(run_tc<LIN_WEIGHT>(p, c, P, st));
         const bool add_db = dbias && db != dbias;
+        if (padded) {
+            launch_k(lin_weight_unpad_kernel, dim3((unsigned)std::min<long long>(ceil_div(n1, 256), p->sms * 8)), dim3(256), 0, st, 1, (const float*)part, c.splits, (long long)co, (int)ci, ci8,
+                     dw);
+            NB_LAUNCH_OK("lin_weight_unpad");
+            return add_db ? sums(nullptr, 0, db, db_parts) : NB_OK;
+        }
         return c.splits > 1 || add_db ? sums(part, c.splits > 1 ? c.splits : 0, db, add_db ? db_parts : 0) : NB_OK;
     }
     LinArgs A;

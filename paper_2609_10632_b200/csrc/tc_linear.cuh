@@ -25,6 +25,7 @@ constexpr uint32_t TL_ONES_BYTES = 4096;
 struct TcLinParams {
     CUtensorMap tmA, tmB, tmOut, tmZ, tmIn;  // tmIn: the residual (forward), z_in (data gradient)
     int M, N, kblocks;  // k-blocks of TL_KC
+    int n_bias;         // columns that have a bias (N may be padded)
     int BN, m_tiles, n_tiles, group_m;
     int stages, acc_stride;
     int nblkB;                     // MN-major: 64-column blocks of this CTA's part of B
@@ -469,7 +470,7 @@ template <typename T, int KIND, bool CG2, int NP> __global__ void __launch_bound
                 };
                 if (KIND == LIN_FWD && p.bias) {
                     __syncwarp();
-                    for (int e = lane; e < ncol; e += 32) my_bias[e] = col0 + e < p.N ? p.bias[col0 + e] : 0.f;
+                    for (int e = lane; e < ncol; e += 32) my_bias[e] = col0 + e < p.n_bias ? p.bias[col0 + e] : 0.f;
                     __syncwarp();
                 }
                 if (in_tma && lane == 0) {

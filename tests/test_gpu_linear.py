@@ -60,6 +60,10 @@ class Case:
         mask[self.off : self.off + v.shape[0] * v.ld].view(v.shape[0], v.ld)[:, : v.shape[1]] = False
         assert (v.buf[mask] == 7.0).all(), f"{name}: written outside the matrix"
 
+    def tc(self, call):
+        """Whether the tensor cores do it: misaligned rows of even layers are left to the CUDA cores."""
+        return self.plan.paths(self.rows)[call] == 1 and (self.ci % 8 != 0 or self.co % 8 != 0 or (self.pad % 8 == 0 and self.off % 8 == 0))
+
     def E(self, a, b, K, tc):
         return ((K / 8 if tc else K) + 16) * 2.0**-24 * (np.abs(a) @ np.abs(b))
 
@@ -82,7 +86,7 @@ class Case:
         self.plan.poll()
         hb = self.bias.double().cpu().numpy() if bias else None
         wz, wout = ora.linear_fwd(self.hx, self.hw, hb, kind, hr)
-        E = self.E(self.hx, self.hw.T, self.ci, self.plan.paths(self.rows)["fwd"] == 1 and self.pad % 8 == 0 and self.off % 8 == 0)
+        E = self.E(self.hx, self.hw.T, self.ci, self.tc("fwd"))
         E = E + 2.0**-23 * (np.abs(wz) + (0 if hb is None else np.abs(hb)))  # the bias added in fp32
         a = {"none": 0.0, "gelu": 2e-5 if self.f16 else 2.8e-4, "silu": 2.5e-4}[kind] if not self.f32 else 2.0**-20
         self.close("out", out, wout, 1.13 * E + a * np.abs(wz) + self.u * np.abs(wout) + 2.0**-22 * (np.abs(wz) + (0 if hr is None else np.abs(hr))))
@@ -100,7 +104,7 @@ class Case:
         self.nb.nb_linear_bwd_data(self.plan, self.rows, self.dy, self.w, dx, self.ws, z_in=z, act_in=KIND[kind], add=ad, ld_dy=self.dy.ld, ld_dx=dx.ld, ld_add=ad.ld if add else 0)
         self.plan.poll()
         want, raw = ora.linear_bwd_data(self.hdy, self.hw, hz, kind, had), np.abs(ora.linear_bwd_data(self.hdy, self.hw, None, "none", had))
-        E = self.E(self.hdy, self.hw, self.co, self.plan.paths(self.rows)["data"] == 1 and self.pad % 8 == 0 and self.off % 8 == 0)
+        E = self.E(self.hdy, self.hw, self.co, self.tc("data"))
         E = E + 2.0**-23 * (raw + (0 if had is None else np.abs(had)))
         slope = np.ones(1) if hz is None else np.abs(ora.act_grad(hz, kind))
         e = 0.0 if hz is None else 2.0**-20 if self.f32 else 4e-5 if kind == "gelu" else 2.5e-4 * (1 + np.abs(hz))
@@ -114,7 +118,7 @@ class Case:
         self.nb.nb_linear_bwd_weight(self.plan, self.rows, self.x, self.dy, dw, db, self.ws, ld_x=self.x.ld, ld_dy=self.dy.ld)
         self.plan.poll()
         wdw, wdb = ora.linear_bwd_weight(self.hx, self.hdy)
-        tc = self.plan.paths(self.rows)["weight"] == 1 and self.pad % 8 == 0 and self.off % 8 == 0
+        tc = self.tc("weight")
         n = self.co * self.ci
         self.close("dw", dw[:n].view(self.co, self.ci), wdw, self.E(self.hdy.T, self.hx, self.rows, tc) + 2.0**-24 * np.abs(wdw))
         assert (dw[n:] == 7.0).all()
@@ -153,6 +157,22 @@ def test_cuda_core_shapes(rows, ci, co, dtype, flags):
 @pytest.mark.parametrize("rows, ci, co", [(5, 1001, 77), (100, 20, 36), (33, 77, 129)])
 def test_odd_channel_counts_in_16_bits(rows, ci, co):
     Case(rows, ci, co, "bf16", seed=1).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows, ci, co, pad, off", [(1100, 333, 401, 0, 0), (700, 1001, 200, 3, 1), (2000, 264, 259, 0, 0), (130, 1003, 1037, 1, 0), (5000, 77, 363, 5, 2)])
+def test_odd_channel_counts_on_padded_copies(rows, ci, co, pad, off, dtype):
+    """From 2^27 products on, layers of odd channel counts take the tensor cores: everything an epilogue can be given, pitches included."""
+    c = Case(rows, ci, co, dtype, seed=rows, pad=pad, off=off)
+    assert c.plan.paths(rows) == {"fwd": 1, "data": 1, "weight": 1}
+    c.forward()
+    c.forward("gelu", res=True, keep_z=True)
+    c.forward("silu", bias=False, res=True, in_place=True)
+    c.data()
+    c.data("gelu", add=True)
+    c.data("silu", add=True, in_place=True)
+    c.weight()
+    c.weight(bias=False)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
