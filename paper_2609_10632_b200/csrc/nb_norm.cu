@@ -1,5 +1,6 @@
 // C ABI of the layer norm (see include/nb_norm.h).  Everything runs on the current device; no memory is allocated.
 #include <algorithm>
+#include <atomic>
 #include <cstring>
 
 #include "../../include/nb_norm.h"
@@ -51,9 +52,34 @@ template <typename T, int V, int VPL> void launch_fwd_lanes(const Group& G, cons
     else launch_k(layer_norm_fwd_kernel<T, V, 0, VPL>, dim3(grid), dim3(G.threads), 0, st, 1, P);
 }
 
-template <typename T> nb_status run_fwd(LnFwd P, bool vec, cudaStream_t st) {
+// Rows that are whole vectors only several at a time: dense, from 16-byte aligned pointers, as wide as the tiles' shared memory and a
+// thread's columns allow.
+constexpr size_t LN_TILE_SMEM = 98304;
+template <typename T> bool tile_rows(bool dense, int c, int tiles, size_t* smem) {
+    *smem = (size_t)tiles * ln_tile_rows<T>() * c * sizeof(T);
+    return dense && c >= 64 && c <= LN_TILE_COLS * LN_TILE_THREADS && *smem <= LN_TILE_SMEM;
+}
+// The tiles may be more shared memory than a kernel has by default: asked for once per kernel and device.
+template <typename... A> nb_status allow_smem(void (*kernel)(A...), std::atomic<unsigned long long>& done) {
+    int dev = 0;
+    cudaGetDevice(&dev);
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (done.load(std::memory_order_acquire) & bit) return NB_OK;
+    NB_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)LN_TILE_SMEM));
+    done.fetch_or(bit, std::memory_order_release);
+    return NB_OK;
+}
+
+template <typename T> nb_status run_fwd(LnFwd P, bool vec, bool dense, cudaStream_t st) {
     constexpr int V = 16 / (int)sizeof(T);
     P.nvec = vec ? P.c / V : P.c;
+    size_t smem = 0;
+    if (!vec && tile_rows<T>(dense, P.c, 1, &smem)) {
+        static std::atomic<unsigned long long> done{0};
+        NB_TRY(allow_smem(layer_norm_fwd_tile_kernel<T>, done));
+        launch_k(layer_norm_fwd_tile_kernel<T>, dim3(blocks_for(P.rows, ln_tile_rows<T>())), dim3(LN_TILE_THREADS), smem, st, 1, P);
+        return launch_ok("layer_norm_fwd (tiles)");
+    }
     if (vec && P.nvec <= 4 * 512) {
         const Group G = choose_group(P.nvec, 4);
         if (G.vpl == 1) launch_fwd_lanes<T, V, 1>(G, P, st);
@@ -99,12 +125,23 @@ template <typename T, int V, int VPL> void launch_bwd_lanes(const Group& G, cons
     else launch_bwd_group<T, V, 0, VPL>(P, grid, G.threads, st);
 }
 
-template <typename T> nb_status run_bwd(LnBwd P, bool vec, int blocks, float* dgamma, float* dbeta, cudaStream_t st) {
+template <typename T> nb_status run_bwd(LnBwd P, bool vec, bool dense, int blocks, float* dgamma, float* dbeta, cudaStream_t st) {
     constexpr int V = 16 / (int)sizeof(T);
     P.nvec = vec ? P.c / V : P.c;
     int parts = blocks;
+    size_t smem = 0;
     constexpr int most = 16 / V;  // 16 columns a thread: their sums, this row's and the next row's values fit 128 registers
-    if (vec && P.nvec <= most * LN_BWD_MAX_BLOCK) {
+    if (!vec && tile_rows<T>(dense, P.c, P.add ? 3 : 2, &smem)) {
+        parts = (int)std::min<long long>(blocks, (P.rows + ln_tile_rows<T>() - 1) / ln_tile_rows<T>());
+        static std::atomic<unsigned long long> done{0}, done_sums{0};
+        if (P.partials) {
+            NB_TRY(allow_smem(layer_norm_bwd_tile_kernel<T, true>, done_sums));
+            launch_k(layer_norm_bwd_tile_kernel<T, true>, dim3((unsigned)parts), dim3(LN_TILE_THREADS), smem, st, 1, P);
+        } else {
+            NB_TRY(allow_smem(layer_norm_bwd_tile_kernel<T, false>, done));
+            launch_k(layer_norm_bwd_tile_kernel<T, false>, dim3((unsigned)parts), dim3(LN_TILE_THREADS), smem, st, 1, P);
+        }
+    } else if (vec && P.nvec <= most * LN_BWD_MAX_BLOCK) {
         const Group G = choose_group(P.nvec, most);
         const int groups = G.lanes ? LN_THREADS / G.lanes : 1;
         parts = (int)std::min<long long>(blocks, (P.rows + groups - 1) / groups);
@@ -139,12 +176,14 @@ nb_status check_rows(int32_t dtype, int64_t rows, int32_t c) {
     if (c > (1 << 24)) return fail(NB_ERR_INVALID_ARG, "c must not be above 2^24");
     return NB_OK;
 }
-// A matrix operand: pitch (0 = dense) and alignment; `vec` stays true while every row is whole 16-byte vectors.
-nb_status check_matrix(const char* name, const void* p, int64_t* ld, int32_t c, size_t es, bool* vec) {
+// A matrix operand: pitch (0 = dense) and alignment; `vec` stays true while every row is whole 16-byte vectors, `dense` while
+// rows follow one another from a 16-byte boundary.
+nb_status check_matrix(const char* name, const void* p, int64_t* ld, int32_t c, size_t es, bool* vec, bool* dense) {
     if (*ld == 0) *ld = c;
     if (*ld < c) return fail(NB_ERR_INVALID_ARG, "ld_%s is smaller than c", name);
     if (reinterpret_cast<uintptr_t>(p) & (es - 1)) return fail(NB_ERR_ALIGNMENT, "%s is not aligned to its element size", name);
     if ((reinterpret_cast<uintptr_t>(p) & 15u) || ((uint64_t)*ld * es) % 16 || ((uint64_t)c * es) % 16) *vec = false;
+    if ((reinterpret_cast<uintptr_t>(p) & 15u) || *ld != c) *dense = false;
     return NB_OK;
 }
 nb_status check_floats(const char* name, const float* p, bool* vec) {
@@ -165,18 +204,18 @@ nb_status nb_layer_norm_fwd(int32_t dtype, int64_t rows, int32_t c, const void* 
     if (!mean != !rstd) return fail(NB_ERR_INVALID_ARG, "mean and rstd must be given together");
     if (!(eps > 0.f)) return fail(NB_ERR_INVALID_ARG, "eps must be positive");
     const size_t es = size_of(dtype);
-    bool vec = true;
-    NB_TRY(check_matrix("x", x, &ld_x, c, es, &vec));
-    NB_TRY(check_matrix("y", y, &ld_y, c, es, &vec));
+    bool vec = true, dense = true;
+    NB_TRY(check_matrix("x", x, &ld_x, c, es, &vec, &dense));
+    NB_TRY(check_matrix("y", y, &ld_y, c, es, &vec, &dense));
     NB_TRY(check_floats("gamma", gamma, &vec));
     NB_TRY(check_floats("beta", beta, &vec));
     NB_TRY(check_floats("mean", mean, nullptr));
     NB_TRY(check_floats("rstd", rstd, nullptr));
     LnFwd P = {x, y, gamma, beta, mean, rstd, rows, ld_x, ld_y, c, 0, eps};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == NB_DTYPE_F32) return run_fwd<float>(P, vec, st);
-    if (dtype == NB_DTYPE_BF16) return run_fwd<__nv_bfloat16>(P, vec, st);
-    return run_fwd<__half>(P, vec, st);
+    if (dtype == NB_DTYPE_F32) return run_fwd<float>(P, vec, dense, st);
+    if (dtype == NB_DTYPE_BF16) return run_fwd<__nv_bfloat16>(P, vec, dense, st);
+    return run_fwd<__half>(P, vec, dense, st);
 }
 
 nb_status nb_layer_norm_workspace_bytes(int64_t rows, int32_t c, size_t* bytes) {
@@ -195,11 +234,11 @@ nb_status nb_layer_norm_bwd(int32_t dtype, int64_t rows, int32_t c, const void* 
     if (!g || !x || !mean || !rstd || !dx) return fail(NB_ERR_INVALID_ARG, "g, x, mean, rstd and dx must not be NULL");
     if (!dgamma != !dbeta) return fail(NB_ERR_INVALID_ARG, "dgamma and dbeta must be given together");
     const size_t es = size_of(dtype);
-    bool vec = true;
-    NB_TRY(check_matrix("g", g, &ld_g, c, es, &vec));
-    NB_TRY(check_matrix("x", x, &ld_x, c, es, &vec));
-    if (add) NB_TRY(check_matrix("add", add, &ld_add, c, es, &vec));
-    NB_TRY(check_matrix("dx", dx, &ld_dx, c, es, &vec));
+    bool vec = true, dense = true;
+    NB_TRY(check_matrix("g", g, &ld_g, c, es, &vec, &dense));
+    NB_TRY(check_matrix("x", x, &ld_x, c, es, &vec, &dense));
+    if (add) NB_TRY(check_matrix("add", add, &ld_add, c, es, &vec, &dense));
+    NB_TRY(check_matrix("dx", dx, &ld_dx, c, es, &vec, &dense));
     NB_TRY(check_floats("gamma", gamma, &vec));
     NB_TRY(check_floats("mean", mean, nullptr));
     NB_TRY(check_floats("rstd", rstd, nullptr));
@@ -209,9 +248,9 @@ nb_status nb_layer_norm_bwd(int32_t dtype, int64_t rows, int32_t c, const void* 
     if (dgamma) NB_TRY(check_ws(workspace, workspace_bytes, align_up((size_t)blocks * 2 * (size_t)c * sizeof(float), 256)));
     LnBwd P = {g, x, add, dx, gamma, mean, rstd, dgamma ? static_cast<float*>(workspace) : nullptr, rows, ld_g, ld_x, ld_add, ld_dx, c, 0};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == NB_DTYPE_F32) return run_bwd<float>(P, vec, blocks, dgamma, dbeta, st);
-    if (dtype == NB_DTYPE_BF16) return run_bwd<__nv_bfloat16>(P, vec, blocks, dgamma, dbeta, st);
-    return run_bwd<__half>(P, vec, blocks, dgamma, dbeta, st);
+    if (dtype == NB_DTYPE_F32) return run_bwd<float>(P, vec, dense, blocks, dgamma, dbeta, st);
+    if (dtype == NB_DTYPE_BF16) return run_bwd<__nv_bfloat16>(P, vec, dense, blocks, dgamma, dbeta, st);
+    return run_bwd<__half>(P, vec, dense, blocks, dgamma, dbeta, st);
 }
 
 }  // extern "C"
