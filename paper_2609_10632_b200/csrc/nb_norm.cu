@@ -26,13 +26,14 @@ size_t size_of(int32_t dtype) { return dtype == NB_DTYPE_F32 ? 4 : 2; }
 struct Group {
     int lanes, vpl, threads;
 };
-// Least idle lanes; among equals the smaller group with more vectors a lane (fewer steps of the reductions).  `most` vectors a lane.
-Group choose_group(int nvec, int most) {
+// Least idle lanes; among equals the smaller group with more vectors a lane (fewer steps of the reductions) or, `wide`, the larger
+// (fewer registers a thread, more blocks an SM: the backward pass over 409600 x 96 bf16 64 -> 60 us).  `most` vectors a lane.
+Group choose_group(int nvec, int most, bool wide) {
     Group best = {0, 0, 0};
     int waste = 1 << 30;
     for (int lanes = 4; lanes <= 32; lanes *= 2)
         for (int vpl = 1; vpl <= most; ++vpl)
-            if (lanes * vpl >= nvec && lanes * vpl - nvec < waste) {
+            if (lanes * vpl >= nvec && lanes * vpl - nvec < waste + (wide ? 1 : 0)) {
                 waste = lanes * vpl - nvec;
                 best = {lanes, vpl, LN_THREADS};
             }
@@ -81,7 +82,7 @@ template <typename T> nb_status run_fwd(LnFwd P, bool vec, bool dense, cudaStrea
         return launch_ok("layer_norm_fwd (tiles)");
     }
     if (vec && P.nvec <= 4 * 512) {
-        const Group G = choose_group(P.nvec, 4);
+        const Group G = choose_group(P.nvec, 4, false);
         if (G.vpl == 1) launch_fwd_lanes<T, V, 1>(G, P, st);
         else if (G.vpl == 2) launch_fwd_lanes<T, V, 2>(G, P, st);
         else if (G.vpl == 3) launch_fwd_lanes<T, V, 3>(G, P, st);
@@ -142,7 +143,7 @@ template <typename T> nb_status run_bwd(LnBwd P, bool vec, bool dense, int block
             launch_k(layer_norm_bwd_tile_kernel<T, false>, dim3((unsigned)parts), dim3(LN_TILE_THREADS), smem, st, 1, P);
         }
     } else if (vec && P.nvec <= most * LN_BWD_MAX_BLOCK) {
-        const Group G = choose_group(P.nvec, most);
+        const Group G = choose_group(P.nvec, most, true);
         const int groups = G.lanes ? LN_THREADS / G.lanes : 1;
         parts = (int)std::min<long long>(blocks, (P.rows + groups - 1) / groups);
         if (G.vpl == 1) launch_bwd_lanes<T, V, 1>(G, P, (unsigned)parts, st);

@@ -169,7 +169,7 @@ template <typename T, int V, int L, int VPL> __global__ void __launch_bounds__(L
 // Dense rows of a channel count that no vector divides: eight of 16-bit elements (four of fp32) are whole 16-byte vectors together,
 // so a block takes that many at a time through shared memory, with vectors from and to global memory.  Warps have the rows for
 // the statistics, threads the columns for the rest.  5003 x 1001 fp16, forward and backward with the sums: 72 us element by element,
-// 41 in this form.
+// 39 in this form.
 constexpr int LN_TILE_THREADS = 256;
 constexpr int LN_TILE_COLS = 8;  // columns of the sums that a thread of the backward pass may own
 template <typename T> __host__ __device__ constexpr int ln_tile_rows() { return 16 / (int)sizeof(T); }
@@ -216,14 +216,17 @@ template <typename T> __global__ void __launch_bounds__(LN_TILE_THREADS) layer_n
         if (warp < R) {
             T* row = t + warp * P.c;
             float s = 0.f;
+#pragma unroll 8
             for (int i = lane; i < P.c; i += 32) s += to_f32<T>(row[i]);
             const float mean = ln_sum<32>(s, nullptr) * inv_c;
             s = 0.f;
+#pragma unroll 8
             for (int i = lane; i < P.c; i += 32) {
                 const float d = to_f32<T>(row[i]) - mean;
                 s = fmaf(d, d, s);
             }
             const float rstd = 1.f / sqrtf(ln_sum<32>(s, nullptr) * inv_c + P.eps);
+#pragma unroll 8
             for (int i = lane; i < P.c; i += 32)
                 row[i] = from_f32<T>(fmaf((to_f32<T>(row[i]) - mean) * rstd, P.gamma ? __ldg(P.gamma + i) : 1.f, P.beta ? __ldg(P.beta + i) : 0.f));
             if (P.mean && lane == 0 && r0 + warp < P.rows) {
@@ -276,7 +279,7 @@ struct LnBwd {
 // Bound: memory (g and x once, dx once).  A block walks over rows; a thread keeps the sums of its own columns in registers, and the
 // next row's g and x are requested before this row's sums are formed.
 template <typename T, int V, int L, int VPL, bool ADD, bool SUMS>
-__global__ void __launch_bounds__(L == 0 ? LN_BWD_MAX_BLOCK : LN_THREADS) layer_norm_bwd_kernel(LnBwd P) {
+__global__ void __launch_bounds__(L == 0 ? LN_BWD_MAX_BLOCK : LN_THREADS, L != 0 && VPL * V <= 8 ? 3 : 1) layer_norm_bwd_kernel(LnBwd P) {
     pdl_launch_dependents();
     pdl_wait();
     __shared__ float2 red[2][32];
@@ -441,6 +444,7 @@ template <typename T, bool SUMS> __global__ void __launch_bounds__(LN_TILE_THREA
             const bool live = r0 + warp < P.rows;
             const float mean = live ? P.mean[r0 + warp] : 0.f, rstd = live ? P.rstd[r0 + warp] : 0.f;
             float2 s = make_float2(0.f, 0.f);
+#pragma unroll 8
             for (int i = lane; i < P.c; i += 32) {
                 const float d = to_f32<T>(g[warp * P.c + i]) * (P.gamma ? __ldg(P.gamma + i) : 1.f);
                 s.x += d;
