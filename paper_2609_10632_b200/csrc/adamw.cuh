@@ -438,10 +438,6 @@ __device__ __forceinline__ void aw_walk32(const AwChunk* C, int from, int to, bo
 }
 
 // The chunks of 8-bit moments: a warp owns 256 consecutive elements of a chunk (two blocks of 128) and a ring in shared memory of
-// its own, into which its share of the two chunks behind the current one travels by asynchronous copies.  The arithmetic takes
-// about as many issue slots as the bytes take time, so the loads have to run beside it: with loads into registers ahead of the
-// arithmetic a step of 101 million parameters takes 426 us, with the ring @@.
-// The chunks of 8-bit moments: a warp owns 256 consecutive elements of a chunk (two blocks of 128) and a ring in shared memory of
 // its own, into which its share of the two chunks behind the current one travels by asynchronous copies.  Here the arithmetic
 // takes nearly as many issue slots as the bytes take time, so loads and arithmetic have to overlap.  100.7 million parameters with bf16
 // gradients, clipped (floor 248 us for 1.62 GB): 507 us with a thread's loads in front of its arithmetic, 432 without guards on full chunks,
