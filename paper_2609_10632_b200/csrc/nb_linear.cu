@@ -32,14 +32,19 @@ struct TlCfg {
     double cost = 0;
 };
 
-// Cycles of a stage (128 rows a CTA, BN columns, 64 k): the products, or the operand bytes from L2 at what an SM gets of them.
-double stage_cycles(bool cg2, int bn) {
+// Cycles of a stage (128 rows a CTA, BN columns, 64 k): the products, or the operand bytes from L2 at what an SM gets of them
+// (measured on products of 1024 to 4096 terms: 700 a stage of 256 columns in a pair, 62 bytes a cycle; the weight gradient, whose
+// operands come in twice as many boxes, follows the second pair of figures better: 8192 x 1024 x 1024 24 against 30 us).
+double stage_cycles(bool cg2, int bn, bool weight) {
     const double bytes = 16384.0 + (cg2 ? bn / 2 : bn) * 128.0;
-    return std::max(2.0 * bn, bytes / 55.0);
+    return weight ? std::max(2.0 * bn, bytes / 55.0) : std::max(2.75 * bn, bytes / 62.0);
 }
 
-// Tiles of a forward product or data gradient: the least time of the persistent loop over what the candidates give.
-TlCfg choose_rows(long long M, long long N, long long K, int sms, double epi_instr) {
+// Tiles of a forward product or data gradient: the least time of the persistent loop over what the candidates give.  A tile takes its
+// products or its epilogue, whichever is longer; the epilogue has a part of its own (handing the accumulators over, twice as long
+// between the CTAs of a pair) and `per_col` cycles for each column.  25600 x 384 -> 1536 with GELU and z: 53 and 57 us on pairs with 256 and 192
+// columns, 48 and 49 on single CTAs; the data gradient through GELU 72, 67 and 61, 58; 25600 x 1536 -> 384 34, 29 and 36, 34.
+TlCfg choose_rows(long long M, long long N, long long K, int sms, double per_col) {
     TlCfg best;
     for (int cg2 = 1; cg2 >= 0; --cg2)
         for (int bn = 256; bn >= 64; bn -= 64) {
@@ -50,7 +55,7 @@ TlCfg choose_rows(long long M, long long N, long long K, int sms, double epi_ins
             c.n_tiles = (int)ceil_div(N, bn);
             c.kblocks = (int)ceil_div(K, TL_KC);
             const long long workers = cg2 ? sms / 2 : sms, tiles = (long long)c.m_tiles * c.n_tiles;
-            const double main = c.kblocks * stage_cycles(cg2, bn), epi = bn * epi_instr;
+            const double main = c.kblocks * stage_cycles(cg2, bn, false), epi = (cg2 ? 2800.0 : 1450.0) + bn * per_col;
             c.cost = (double)ceil_div(tiles, workers) * std::max(main, epi) + std::min(main, epi) + 1000.0;
             if (!best.bn || c.cost < best.cost) best = c;
         }
@@ -75,7 +80,7 @@ TlCfg choose_weight(long long M, long long N, long long K, int sms) {
             for (long long s = 1; s <= most; ++s) {
                 c.kb_per_split = (int)ceil_div(c.kblocks, s);
                 c.splits = (int)ceil_div(c.kblocks, c.kb_per_split);
-                const double item = c.kb_per_split * stage_cycles(cg2, bn) + bn * 8.0 + 1500.0;
+                const double item = c.kb_per_split * stage_cycles(cg2, bn, true) + bn * 8.0 + 1500.0;
                 // (slices: written, read back and added at about 2.5 KB a cycle, and another launch)
                 const double sums = c.splits > 1 ? 3000.0 + 2.0 * c.splits * (double)M * N * 4 / 2500.0 : 0.0;
                 const double db = db_in_tile(c) ? 0.0 : 3000.0 + 2.0 * M * K / 3400.0;
@@ -282,7 +287,7 @@ template <typename T> nb_status run_rows(const nb_linear_plan_s* plan, LinArgs& 
 // on operands whose rows are whole vectors; N and K may be padded counts (w has c_out rows all the same)
 nb_status tc_fwd(const nb_linear_plan_s* p, long long rows, const void* x, long long ld_x, const void* w, const float* bias, int act, const void* res, long long ld_res, void* z,
                  void* out, long long ld_out, int ci, int co, cudaStream_t st) {
-    const TlCfg c = choose_rows(rows, co, ci, p->sms, 6.0 + (act ? 10.0 : 0.0) + (z ? 3.0 : 0.0) + (res ? 3.0 : 0.0));
+    const TlCfg c = choose_rows(rows, co, ci, p->sms, 15.0 + (bias ? 3.0 : 0.0) + (act == NB_ACT_GELU ? 8.0 : act ? 4.5 : 0.0) + (z ? 4.0 : 0.0) + (res ? 10.0 : 0.0));
     TcLinParams P;
     memset(&P, 0, sizeof P);
     P.M = (int)rows; P.N = co; P.n_bias = p->d.c_out;
@@ -296,7 +301,7 @@ nb_status tc_fwd(const nb_linear_plan_s* p, long long rows, const void* x, long 
 }
 nb_status tc_data(const nb_linear_plan_s* p, long long rows, const void* dy, long long ld_dy, const void* w, const void* z_in, int act_in, const void* add, long long ld_add, void* dx,
                   long long ld_dx, int ci, int co, cudaStream_t st) {
-    const TlCfg c = choose_rows(rows, ci, co, p->sms, 6.0 + (z_in ? 16.0 : 0.0) + (add ? 3.0 : 0.0));
+    const TlCfg c = choose_rows(rows, ci, co, p->sms, 15.0 + (act_in == NB_ACT_GELU ? 24.0 : z_in ? 14.0 : 0.0) + (add ? 10.0 : 0.0));
     TcLinParams P;
     memset(&P, 0, sizeof P);
     P.M = (int)rows; P.N = ci;

@@ -491,7 +491,7 @@ template <typename T, int KIND, bool CG2, int NP> __global__ void __launch_bound
                     if (in_tma) {  // (waited for whatever has failed: nothing may land after the CTA has exited)
                         __syncwarp();
                         bool there = false;
-                        for (int j = 0; j < 4000000 && !(there = ptx::mbar_try_wait(my_in + buf, (in_ph >> buf) & 1u)); ++j) {
+                        for (int j = 0; j < 400000 && !(there = ptx::mbar_try_wait(my_in + buf, (in_ph >> buf) & 1u)); ++j) {
                         }
                         ok = __all_sync(0xffffffffu, ok && there) != 0;
                         in_ph ^= 1u << buf;
