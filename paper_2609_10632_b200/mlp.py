@@ -47,13 +47,21 @@ class MlpBlock:
                 self.copy[k].copy_(self.param[k])
 
     def forward(self, stream=None):
+        with torch.cuda.device(self.dev):  # (the norm's calls have no plan: they run on the current device)
+            self._forward(stream)
+
+    def backward(self, stream=None):
+        """All gradients and dx from dy; the gradient of the residual joins in the norm's backward pass."""
+        with torch.cuda.device(self.dev):
+            self._backward(stream)
+
+    def _forward(self, stream):
         p = self.param
         nb.nb_layer_norm_fwd(self.dtype, self.rows, self.c, self.x, p["gamma"], p["beta"], self.eps, self.h, self.mean, self.rstd, stream=stream)
         nb.nb_linear_fwd(self.up, self.rows, self.h, self.copy["w1"], p["b1"], self.act, self.a, self.ws, z=self.z, stream=stream)
         nb.nb_linear_fwd(self.down, self.rows, self.a, self.copy["w2"], p["b2"], nb.NB_ACT_NONE, self.y, self.ws, res=self.x, stream=stream)
 
-    def backward(self, stream=None):
-        """All gradients and dx from dy; the gradient of the residual joins in the norm's backward pass."""
+    def _backward(self, stream):
         g = self.grad
         nb.nb_linear_bwd_weight(self.down, self.rows, self.a, self.dy, g["w2"], g["b2"], self.ws, stream=stream)
         nb.nb_linear_bwd_data(self.down, self.rows, self.dy, self.copy["w2"], self.dz, self.ws, z_in=self.z, act_in=self.act, stream=stream)
