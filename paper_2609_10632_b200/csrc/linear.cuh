@@ -51,7 +51,7 @@ __device__ __forceinline__ float2 lin_tanh2(float2 h) {
 }
 // T = bf16: GELU by z/2 (1 + tanh(z (a + b z^2 + c z^4))) with coefficients fitted here to GELU itself (|error| of the fit <= 2.6e-5) and the
 // hardware's tanh (2^-10.987, relative): 2.8e-4 |z| in all, an eighth of what rounding a bf16 result of order one takes, for half the
-// arithmetic of the polynomial: 25600 x 384 -> 1536 with z 61 us with that, 56 with this.  fp16 results keep the polynomial.
+// arithmetic of the polynomial: 25600 x 384 -> 1536 with z, on pairs of CTAs, 61 us with that, 56 with this; 51 on the tiles chosen now.  fp16 results keep the polynomial.
 template <typename T> __device__ __forceinline__ float2 lin_act2(float2 z, int act) {
     if (act == NB_ACT_GELU && sizeof(T) == 2 && !std::is_same<T, __half>::value) {
         float2 u = mul2(z, z);
