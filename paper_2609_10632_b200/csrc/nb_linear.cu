@@ -77,7 +77,8 @@ TlCfg choose_weight(long long M, long long N, long long K, int sms) {
             c.kblocks = (int)ceil_div(K, TL_KC);
             const long long workers = cg2 ? sms / 2 : sms, tiles = (long long)c.m_tiles * c.n_tiles;
             const long long most = std::max<long long>(1, std::min<long long>({64, c.kblocks, ceil_div(4 * workers, tiles)}));
-            for (long long s = 1; s <= most; ++s) {
+            // (from one length of a slice to the next shorter one: counts that give the same length give the same slices, and every call asks)
+            for (long long s = 1; s <= most; s = c.kb_per_split > 1 ? ceil_div(c.kblocks, c.kb_per_split - 1) : most + 1) {
                 c.kb_per_split = (int)ceil_div(c.kblocks, s);
                 c.splits = (int)ceil_div(c.kblocks, c.kb_per_split);
                 const double item = c.kb_per_split * stage_cycles(cg2, bn, true) + bn * 8.0 + 1500.0;
