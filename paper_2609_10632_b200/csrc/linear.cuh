@@ -125,9 +125,10 @@ template <typename T, int KIND> __device__ __forceinline__ void lin_store(const 
 }
 
 // Bound: FMA issue.  A block of 256 threads has a [TILE x TILE] tile: 128 (a thread [8 x 8]: four 16-byte shared loads for 64 products) where
-// there are enough of them, else 64 ([4 x 4]), with slices of k that put four blocks on an SM.  Operand tiles of 16 k travel
+// there are enough of them, on their own or with long slices of k, else 64 ([4 x 4]), with slices that put four blocks on an SM.  Operand tiles of 16 k travel
 // through registers into shared memory as fp32, k-major, double-buffered.  VEC: every operand row is whole vectors of four.
 // 1600 x 384 x 384 forward: 43 us with one 64-tile block an SM, 37 with four; 8000 x 1024 x 1024 480 us (35 TFLOP/s; the library product 360).
+// 1061 x 3520 -> 1000 forward: 369 us on tiles of 64, 213 on tiles of 128 in four slices; the weight gradient of 25600 x 384 -> 384 285 and 148.
 constexpr int LS_BK = 16, LS_THREADS = 256;
 
 // Four elements of an operand stored [outer][inner] at (outer, inner..inner+3) as fp32, zeros outside.

@@ -102,10 +102,13 @@ SimtCfg simt_cfg(long long M, long long N, long long K, int sms, bool weight) {
     SimtCfg c;
     c.tiles = ceil_div(M, 128) * ceil_div(N, 128);
     long long s = 1;
-    if (2 * c.tiles >= 3 * sms) {
+    const long long small = ceil_div(M, 64) * ceil_div(N, 64), s128 = c.tiles < 2 * sms ? 2 * sms / c.tiles : 1;
+    // Tiles of 128 while they, with slices of 256 products or more each, are two on most SMs, and their edges no large part of them.
+    if (2 * c.tiles * s128 >= 3 * sms && (s128 == 1 || (K / s128 >= 256 && 8 * c.tiles <= 3 * small))) {
         c.tile = 128;
+        s = s128;
     } else {
-        c.tiles = ceil_div(M, 64) * ceil_div(N, 64);
+        c.tiles = small;
         // as many slices as give an SM four blocks, of 64 products or more each
         if (c.tiles < 4 * sms) s = std::min<long long>(ceil_div(4 * sms, c.tiles), std::max<long long>(1, K / 64));
     }
