@@ -154,6 +154,13 @@ def test_cuda_core_shapes(rows, ci, co, dtype, flags):
     c.all()
 
 
+@pytest.mark.parametrize("dtype, flags", [("f32", 0), ("bf16", 1)])
+@pytest.mark.parametrize("rows, ci, co", [(300, 3500, 1001), (7000, 500, 380), (1061, 1003, 3520)])
+def test_cuda_core_large_tiles_with_slices(rows, ci, co, dtype, flags):
+    """Few tiles of 128 and long sums: the forward product, the weight gradient and the data gradient, each in slices of k."""
+    Case(rows, ci, co, dtype, seed=co, flags=flags).all()
+
+
 @pytest.mark.parametrize("rows, ci, co", [(5, 1001, 77), (100, 20, 36), (33, 77, 129)])
 def test_odd_channel_counts_in_16_bits(rows, ci, co):
     Case(rows, ci, co, "bf16", seed=1).all()
