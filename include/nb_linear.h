@@ -13,8 +13,8 @@
  * epilogue works on the fp32 sums and rounds once (z and out each once, from the same sum); fp16 stores saturate at +-65504.
  *   NB_DTYPE_BF16 / NB_DTYPE_F16: tcgen05 tensor cores where c_in and c_out are multiples of 8 and pitches and pointers whole
  *     16-byte vectors, and on padded copies (in the workspace) of layers with other channel counts from 2^27 products on
- *     (nb_linear_paths); CUDA cores elsewhere.  On the tensor cores Phi is a polynomial (|error| <= 2e-5; in
- *     a bf16 forward pass by the hardware's tanh, 2.8e-4) and the logistic function by the hardware's tanh (2.5e-4).
+ *     (nb_linear_paths); CUDA cores elsewhere.  There the activations are those of fp32; on the tensor cores they are approximated, with
+ *     errors relative to the value in the tails too: Phi(z) and GELU within 2^-15 for |z| <= 8, the logistic function and SiLU within 2^-18.
  *   NB_DTYPE_F32: plain FMA arithmetic (no TF32).
  * Sums have a fixed order: results are bitwise reproducible on a given device for the same shapes and alignment.
  *

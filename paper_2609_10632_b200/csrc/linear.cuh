@@ -2,8 +2,6 @@
 // for the arithmetic; the tensor-core kernel is tc_linear.cuh).
 #pragma once
 #include "../../include/nb_linear.h"
-#include <type_traits>
-
 #include "common.cuh"
 
 namespace nbcbs {
@@ -26,61 +24,63 @@ __device__ __forceinline__ float lin_act_grad(float z, int act) {
 }
 
 // ------------------------------------------------------------------------------------------ the same for 16-bit results
-// Phi(z) - 1/2 of two values: an odd polynomial of degree 17 on [-4.2, 4.2], fitted here (least squares with Lawson's weights, its
-// end held at 1/2, the last bits of two coefficients such that it comes out as exactly 1/2 there in fp32: beyond, GELU is 0 or z),
-// |error| <= 1.6e-5 in fp32.  No special-function unit: that one is half as fast as the epilogue of a product with few terms needs.
-__device__ __forceinline__ float2 lin_phi2(float2 z) {
-    z.x = fminf(fmaxf(z.x, -4.2f), 4.2f);
-    z.y = fminf(fmaxf(z.y, -4.2f), 4.2f);
-    const float2 u = mul2(z, z);
-    float2 p = fma2(u, splat2(6.210412045737357e-11f), splat2(-5.7821978316496825e-09f));
-    p = fma2(p, u, splat2(2.386405242305045e-07f));
-    p = fma2(p, u, splat2(-5.825401785841677e-06f));
-    p = fma2(p, u, splat2(9.512664109934121e-05f));
-    p = fma2(p, u, splat2(-0.0011167984921485186f));
-    p = fma2(p, u, splat2(0.009836794808506966f));
-    p = fma2(p, u, splat2(-0.06636781245470047f));
-    p = fma2(p, u, splat2(0.3989095687866211f));
-    return mul2(p, z);
+// Errors relative to the VALUE, in the tails too: GELU and SiLU of a negative z are far smaller than z, and an absolute error that
+// rounding hides at z = 1 is the whole value at z = -5 (SiLU by the hardware's tanh, which was here, is 10 % off at -6).  So nothing
+// is formed as a difference of nearly equal numbers.  With t = |z|:
+//   E = e^(-t^2/2),  q = Phi(-t) = E * P(1 / (1 + 0.36 t)):  P a polynomial of degree 5 (Hastings' form of the tail), fitted here to
+//   Phi(-t) e^(t^2/2) on [0, 14] for the least relative error, 1.3e-5; with the roundings of E's exponent 2^-15 as far as t = 8
+//   (beyond, E is the error: its exponent's rounding grows as t^2, and 2^-126 is reached at 13.2).
+// t counts as 64 at most, so that 0 * inf is not formed; a NaN stays in E.
+struct LinTail {
+    float2 t, E, minus_P;
+};
+__device__ __forceinline__ float lin_ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
-__device__ __forceinline__ float2 lin_tanh2(float2 h) {
-    float2 t;
-    asm("tanh.approx.f32 %0, %1;" : "=f"(t.x) : "f"(h.x));
-    asm("tanh.approx.f32 %0, %1;" : "=f"(t.y) : "f"(h.y));
-    return t;
+__device__ __forceinline__ float lin_rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
-// T = bf16: GELU by z/2 (1 + tanh(z (a + b z^2 + c z^4))) with coefficients fitted here to GELU itself (|error| of the fit <= 2.6e-5) and the
-// hardware's tanh (2^-10.987, relative): 2.8e-4 |z| in all, an eighth of what rounding a bf16 result of order one takes, for half the
-// arithmetic of the polynomial: 25600 x 384 -> 1536 with z, on pairs of CTAs, 61 us with that, 56 with this; 51 on the tiles chosen now.  fp16 results keep the polynomial.
-template <typename T> __device__ __forceinline__ float2 lin_act2(float2 z, int act) {
-    if (act == NB_ACT_GELU && sizeof(T) == 2 && !std::is_same<T, __half>::value) {
-        float2 u = mul2(z, z);
-        u.x = fminf(u.x, 30.f);  // (the tanh is 1 from there on, and the fit would turn back)
-        u.y = fminf(u.y, 30.f);
-        const float2 p = fma2(fma2(u, splat2(-0.0003515216230880469f), splat2(0.037005677819252014f)), u, splat2(0.7975078225135803f));
-        const float2 h = mul2(z, splat2(0.5f));
-        return fma2(h, lin_tanh2(mul2(z, p)), h);
+__device__ __forceinline__ LinTail lin_tail2(float2 z) {
+    LinTail o;
+    const float2 e = mul2(mul2(z, z), splat2(-0.72134752f));  // -z^2/2 in base 2
+    o.E = make_float2(lin_ex2(e.x), lin_ex2(e.y));
+    o.t = make_float2(fminf(fabsf(z.x), 64.f), fminf(fabsf(z.y), 64.f));
+    const float2 d = fma2(o.t, splat2(0.36f), splat2(1.f));
+    const float r = lin_rcp(d.x * d.y);  // (one reciprocal for both: the special-function unit is what this takes most of)
+    const float2 u = mul2(splat2(r), make_float2(d.y, d.x));
+    float2 p = fma2(u, splat2(0.09851564340977417f), splat2(-0.25438743173341666f));
+    p = fma2(p, u, splat2(-0.035116434501124935f));
+    p = fma2(p, u, splat2(-0.16869575236171047f));
+    p = fma2(p, u, splat2(-0.14012407751013303f));
+    o.minus_P = fma2(p, u, splat2(-0.0001912892156621022f));
+    return o;
+}
+// The logistic function 1 / (1 + e^-z): relative error 2^-19 or less from z = -8 on (the exponent's rounding grows as z; at -87 the sum
+// leaves what the reciprocal takes and the result is zero).
+__device__ __forceinline__ float2 lin_logistic2(float2 z) {
+    const float2 e = mul2(z, splat2(-1.44269504f)), d = add2(make_float2(lin_ex2(e.x), lin_ex2(e.y)), splat2(1.f));
+    return make_float2(lin_rcp(d.x), lin_rcp(d.y));
+}
+__device__ __forceinline__ float2 lin_act2(float2 z, int act) {
+    if (act == NB_ACT_GELU) {  // z Phi(z) = max(z, 0) - t Phi(-t)
+        const LinTail f = lin_tail2(z);
+        return fma2(mul2(f.E, f.minus_P), f.t, make_float2(fmaxf(z.x, 0.f), fmaxf(z.y, 0.f)));
     }
-    if (act == NB_ACT_GELU) return fma2(z, lin_phi2(z), mul2(z, splat2(0.5f)));
-    if (act == NB_ACT_SILU) {
-        const float2 h = mul2(z, splat2(0.5f));
-        return fma2(h, lin_tanh2(h), h);
-    }
+    if (act == NB_ACT_SILU) return mul2(z, lin_logistic2(z));
     return z;
 }
 __device__ __forceinline__ float2 lin_act_grad2(float2 z, int act) {
-    if (act == NB_ACT_GELU) {
-        const float2 e = mul2(mul2(z, z), splat2(-0.72134752f));  // -z^2/2 in base 2
-        float2 d;
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d.x) : "f"(e.x));
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d.y) : "f"(e.y));
-        // (an infinite z would make inf * 0 of the second term: a z beyond 64 counts as 64, where that term is zero)
-        const float2 c = make_float2(fminf(fmaxf(z.x, -64.f), 64.f), fminf(fmaxf(z.y, -64.f), 64.f));
-        return fma2(mul2(c, splat2(0.39894228f)), d, add2(lin_phi2(z), splat2(0.5f)));
+    if (act == NB_ACT_GELU) {  // Phi(z) + z phi(z): with k = t phi(t) - Phi(-t), -k for a negative z and 1 + k else
+        const LinTail f = lin_tail2(z);
+        const float2 k = mul2(f.E, fma2(f.t, splat2(0.39894228f), f.minus_P)), r = add2(k, splat2(1.f));
+        return make_float2(z.x < 0.f ? -k.x : r.x, z.y < 0.f ? -k.y : r.y);
     }
     if (act == NB_ACT_SILU) {
-        const float2 s = fma2(lin_tanh2(mul2(z, splat2(0.5f))), splat2(0.5f), splat2(0.5f));
-        const float2 q = fma2(s, splat2(-1.f), splat2(1.f));
+        const float2 s = lin_logistic2(z), q = fma2(s, splat2(-1.f), splat2(1.f));
         return mul2(s, fma2(z, q, splat2(1.f)));
     }
     return splat2(1.f);

@@ -120,10 +120,10 @@ template <typename T, int KIND, int NP> struct TlPass {
             }
             if (p.act == NB_ACT_GELU) {
 #pragma unroll
-                for (int j = 0; j < NP / 2; ++j) v[j] = lin_act2<T>(v[j], NB_ACT_GELU);
+                for (int j = 0; j < NP / 2; ++j) v[j] = lin_act2(v[j], NB_ACT_GELU);
             } else if (p.act == NB_ACT_SILU) {
 #pragma unroll
-                for (int j = 0; j < NP / 2; ++j) v[j] = lin_act2<T>(v[j], NB_ACT_SILU);
+                for (int j = 0; j < NP / 2; ++j) v[j] = lin_act2(v[j], NB_ACT_SILU);
             }
             if (p.has_in) {
 #pragma unroll
