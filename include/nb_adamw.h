@@ -52,7 +52,7 @@ typedef struct nb_adamw_tensor {
     void* param_copy;         /* NULL, or [numel] 16-bit working copy, rewritten */
     int64_t numel;            /* > 0 */
     int32_t group;            /* 0 .. NB_SGD_GROUPS-1 */
-    int32_t copy_dtype;       /* 0 or NB_DTYPE_BF16 = bf16, NB_DTYPE_F16 = IEEE fp16 (saturating) */
+    int32_t copy_dtype;       /* 0 or NB_DTYPE_BF16 = bf16, NB_DTYPE_F16 = IEEE fp16 (saturating; a NaN stays one) */
     int32_t grad_dtype;       /* nb_dtype */
     int32_t state_bits;       /* 32 or 8; may differ from tensor to tensor of a list */
 } nb_adamw_tensor;

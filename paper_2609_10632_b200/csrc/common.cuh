@@ -48,9 +48,12 @@ template <> __device__ __forceinline__ float to_f32<__half>(__half v) { return _
 template <typename T> __device__ __forceinline__ T from_f32(float v);
 template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
-// fp16 stores saturate instead of producing inf (the saved conv output must stay finite for BN).
+// fp16 stores saturate instead of producing inf (the saved conv output must stay finite for BN).  A NaN stays one (fminf and fmaxf would
+// make it -65504), so that whoever looks for NaN behind a store finds it.
 template <> __device__ __forceinline__ __half from_f32<__half>(float v) {
-    return __float2half_rn(fminf(fmaxf(v, -65504.f), 65504.f));
+    __half_raw h;
+    asm("cvt.rn.satfinite.f16.f32 %0, %1;" : "=h"(h.x) : "f"(v));
+    return __half(h);
 }
 
 // Two fp32 values per instruction (fma / mul / add .f32x2 of sm_100): each half is the IEEE round-to-nearest result of the
@@ -79,7 +82,7 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 }
 __device__ __forceinline__ float2 splat2(float v) { return make_float2(v, v); }
 
-// Elements 2j and 2j+1 of a vector as fp32, and back (round to nearest; fp16 saturates like from_f32<__half>).
+// Elements 2j and 2j+1 of a vector as fp32, and back (round to nearest; fp16 like from_f32<__half>).
 template <typename T> __device__ __forceinline__ float2 pair_to_f32(const T* v);
 template <> __device__ __forceinline__ float2 pair_to_f32<float>(const float* v) { return make_float2(v[0], v[1]); }
 template <> __device__ __forceinline__ float2 pair_to_f32<__nv_bfloat16>(const __nv_bfloat16* v) {
@@ -95,9 +98,7 @@ template <> __device__ __forceinline__ void pair_from_f32<__nv_bfloat16>(__nv_bf
     *reinterpret_cast<__nv_bfloat162*>(v) = __float22bfloat162_rn(f);
 }
 template <> __device__ __forceinline__ void pair_from_f32<__half>(__half* v, float2 f) {
-    f.x = fminf(fmaxf(f.x, -65504.f), 65504.f);
-    f.y = fminf(fmaxf(f.y, -65504.f), 65504.f);
-    *reinterpret_cast<__half2*>(v) = __float22half2_rn(f);
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(*reinterpret_cast<uint32_t*>(v)) : "f"(f.y), "f"(f.x));
 }
 
 // 16-byte vector of VT elements (8 x 16-bit or 4 x fp32).
