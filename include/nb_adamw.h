@@ -13,6 +13,9 @@
  *   copy  = p rounded to bf16 or fp16                  (when the tensor has a 16-bit working copy)
  *   *step = t
  *
+ * Moments are fp32 numbers: without clipping a gradient above about 6e20 has v = inf, whose update is m / inf = 0 (the parameter only
+ * decays), and v of gradients below about 4e-18 is a subnormal number with fewer bits, whose root is taken all the same.
+ *
  * The count of steps lives in DEVICE memory: a step that the loss scaler skips does not count, and a step captured into
  * a CUDA graph goes on counting as it is replayed.
  *

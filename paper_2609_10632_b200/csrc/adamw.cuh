@@ -192,8 +192,8 @@ __global__ void __launch_bounds__(AW_THREADS, AW_BLOCKS_PER_SM) adamw_norm_kerne
 }
 
 // sqrt(v) of two non-negative numbers: the hardware's approximate 1/sqrt, then one step of Newton's method on the residual
-// v - r*r, which a fused multiply-add gives without rounding error.  1/sqrt is cut to 2^63, so that zero comes out as zero; a v
-// below 2^-126 (which the approximation takes for zero) gives a positive number below its root, inf gives NaN.
+// v - r*r, which a fused multiply-add gives without rounding error.  1/sqrt is cut to 2^63, so that zero comes out as zero.  Not for a v
+// between 0 and 2^-126, which the approximation takes for zero, nor for inf.
 __device__ __forceinline__ float2 aw_root(float2 v) {
     float2 y, e;
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(v.x));
@@ -205,6 +205,15 @@ __device__ __forceinline__ float2 aw_root(float2 v) {
     e.y = fmaf(-r.y, r.y, v.y);
     return fma2(mul2(e, splat2(0.5f)), y, r);
 }
+
+// The update of such a v, over the whole range of fp32: approximations of 2^-23 that take subnormal numbers, zero and inf as they are.
+__device__ __forceinline__ float aw_careful(float m, float v, float& root, float step_size, float inv_root_bc2, float eps) {
+    float q;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v));
+    asm("div.full.f32 %0, %1, %2;" : "=f"(q) : "f"(m * -step_size), "f"(fmaf(root, inv_root_bc2, eps)));
+    return q;
+}
+__device__ __forceinline__ bool aw_not_normal(float v) { return __float_as_uint(v) - 0x00800000u >= 0x7f000000u; }
 
 // Two elements: the moments in place (each operation rounded by itself), the new parameters returned.
 __device__ __forceinline__ float2 aw_two(float2 g, float2 p, float2& m, float2& v, float2& root, float coef, float step_size, float inv_root_bc2, float keep, const AwScalars& hs) {
@@ -218,7 +227,12 @@ __device__ __forceinline__ float2 aw_two(float2 g, float2 p, float2& m, float2& 
     float2 rec;  // (within 2^-22, which moves a parameter by 2^-22 of one step)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rec.x) : "f"(den.x));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rec.y) : "f"(den.y));
-    return fma2(p, splat2(keep), mul2(mul2(m, splat2(-step_size)), rec));
+    // A v that is not a normal number (zero, underflown, overflown to inf, NaN) takes another way: the root's tricks do not cover it,
+    // and with a tiny eps neither the reciprocal's.  With inf the update is m / inf = 0.
+    float2 update = mul2(mul2(m, splat2(-step_size)), rec);
+    if (aw_not_normal(v.x)) update.x = aw_careful(m.x, v.x, root.x, step_size, inv_root_bc2, hs.eps);
+    if (aw_not_normal(v.y)) update.y = aw_careful(m.y, v.y, root.y, step_size, inv_root_bc2, hs.eps);
+    return fma2(p, splat2(keep), update);
 }
 
 __device__ __forceinline__ float aw_max_nan(float a, float b) {

@@ -308,3 +308,37 @@ def test_refusals():
         with pytest.raises(nb.NbError):
             nb.AdamWPlan([items])
     assert int(st.step) == 0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_second_moments_beyond_the_range_of_normal_numbers(bits):
+    """Without clipping a finite gradient of 1e21 has an infinite v: m / inf is nothing, the parameter only decays.  A v below 2^-126 has
+    its root all the same, which is what the update divides by where eps is 0 or tiny: against the moments that the step left
+    (32 bits), in fp64, to 1e-5 of the update as elsewhere in this file; v = 0 under an m that is not zero divides by eps alone."""
+    import torch
+
+    g = [1e21, -1e30, 3e38, 1e-18, -3e-19, 1e-19, 2e-20, -1e-20, 0.0, 1e-3, 2e-22, -5e-22] + [0.0] * 116 + [1e-19] * 128
+    for eps in (0.0, 1e-40, 1e-30, 1e-8):
+        st = State([(len(g), 0, bits, "f32", None)], seed=12)
+        x = st.t[0]
+        x["g"].copy_(torch.tensor(g))
+        p0 = x["p"].double().cpu().numpy()
+        st.plan.step(st.ws, st.step, LR, WD, B1, B2, eps, 0.0)
+        torch.cuda.synchronize()
+        p, keep = x["p"].double().cpu().numpy(), 1 - LR[0] * WD[0]
+        assert (np.abs(p[:3] - keep * p0[:3]) <= 2.0**-23 * np.abs(p0[:3])).all(), (eps, p[:3], p0[:3])
+        hg = np.array(g, dtype=np.float32)
+        with np.errstate(over="ignore"):
+            m, v = np.float32(0.1) * hg, (np.float32(0.001) * hg) * hg  # (m and v of a first step, each product rounded once)
+        if bits == 32:
+            m, v = x["m"].cpu().numpy(), x["v"].cpu().numpy()
+        m, v = m.astype(np.float64), v.astype(np.float64)
+        some = (v > 0) & np.isfinite(v) if eps == 0 else np.isfinite(v)
+        some &= ~((v == 0) & (m != 0) & (LR[0] * np.abs(m) * 10 > 1e30 * eps))
+        with np.errstate(all="ignore"):
+            update = LR[0] * (m / (1 - B1)) / (np.sqrt(v / (1 - B2)) + np.float64(np.float32(eps)))
+        assert some.sum() > 130 and np.isfinite(update[some]).all()
+        p, p0, update, nan = p[some], p0[some], update[some], np.isnan(p[8]) and not np.isfinite(p[10:12]).any()
+        assert (np.abs(p - (keep * p0 - update)) <= 1e-5 * np.abs(update) + 2.0**-22 * (np.abs(p0) + np.abs(update))).all(), eps
+        if eps == 0:  # 0 / 0 and m / 0 are what the formula says
+            assert nan
