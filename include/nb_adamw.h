@@ -89,7 +89,7 @@ nb_status nb_adamw_upload(nb_adamw_plan plan, void* workspace, size_t workspace_
 /* One step, ordered on `stream` after the upload.  `step` is a device int64 (8-byte aligned), the number of steps
  * taken so far (initialise to 0).  total_norm (device, may be NULL) receives the gradient norm before clipping; with
  * clipping disabled and total_norm NULL the gradients are read once.  Safe to capture into a CUDA graph.
- * Without a scaler gradients that are inf or NaN reach the parameters.
+ * Without a scaler gradients that are inf or NaN reach the parameters; with clipping a NaN makes c and so every parameter NaN.
  * Errors: NB_ERR_INVALID_ARG, NB_ERR_WORKSPACE, NB_ERR_ALIGNMENT, NB_ERR_CUDA. */
 nb_status nb_adamw_step(nb_adamw_plan plan, void* workspace, size_t workspace_bytes, const nb_adamw_hyper* hyper, int64_t* step,
                         float* total_norm, void* stream);

@@ -572,7 +572,10 @@ __global__ void __launch_bounds__(AW_THREADS, AW_BLOCKS_PER_SM) adamw_update_ker
         const double inv = hs.scaler ? 1.0 / (double)S.loss_scale : 1.0;
         const double total = sqrt(t) * inv;  // inf or NaN if any gradient element is
         double c = 1.0;
-        if (hs.max_norm > 0.f && hs.max_norm < __int_as_float(0x7f800000)) c = fmin((double)hs.max_norm / (total + 1e-6), 1.0);
+        if (hs.max_norm > 0.f && hs.max_norm < __int_as_float(0x7f800000)) {
+            c = (double)hs.max_norm / (total + 1e-6);
+            c = c > 1.0 ? 1.0 : c;  // (a NaN norm stays NaN: no tensor takes an unclipped step)
+        }
         const bool skip = hs.scaler && !isfinite(t);
         s_coef = (float)(c * inv);
         s_skip = skip;

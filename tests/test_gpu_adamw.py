@@ -342,3 +342,22 @@ def test_second_moments_beyond_the_range_of_normal_numbers(bits):
         assert (np.abs(p - (keep * p0 - update)) <= 1e-5 * np.abs(update) + 2.0**-22 * (np.abs(p0) + np.abs(update))).all(), eps
         if eps == 0:  # 0 / 0 and m / 0 are what the formula says
             assert nan
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_nan_gradient_makes_the_clipped_step_nan(bits):
+    """The norm is NaN, so min(max_norm / (norm + 1e-6), 1) is: no tensor takes an unclipped step.  An infinite gradient clips all others to nothing."""
+    import torch
+
+    for bad in (float("nan"), float("inf")):
+        st = State([(300, 0, bits, "f32", None), (5000, 1, bits, "bf16", None)], seed=13)
+        st.grads(5.0)
+        st.t[0]["g"][7] = bad
+        before = st.t[1]["p"].clone()
+        st.plan.step(st.ws, st.step, LR, WD, B1, B2, EPS, 1.0, total_norm=st.norm)
+        torch.cuda.synchronize()
+        assert st.t[0]["p"][7].isnan() and not np.isfinite(float(st.norm))
+        if bad != bad:
+            assert st.t[0]["p"].isnan().all() and st.t[1]["p"].isnan().all()
+        else:
+            assert torch.equal(st.t[1]["p"], before)  # (group 1 has no decay)
