@@ -495,7 +495,7 @@ def _refuse(message, status=NB_ERR_INVALID_ARG):
 class AdamWPlan:
     """Owner of one nb_adamw_plan handle.  `tensors`: iterable of (grad, param, exp_avg, exp_avg_sq, param_copy or None, group) of
     contiguous device tensors, with (exp_avg_scale, exp_avg_sq_scale) behind them where the moments are held in 8 bits
-    (torch.float8_e4m3fn or torch.uint8, one fp32 scale for each 128 elements)."""
+    (torch.float8_e4m3fn or torch.uint8, one fp32 scale for each 128 elements).  The plan keeps them until it is closed."""
 
     def __init__(self, tensors, device=0):
         items = [tuple(it) for it in tensors]
@@ -516,7 +516,7 @@ class AdamWPlan:
                     _refuse(f"tensor {i}: {name} must be {count} contiguous elements of {' or '.join(dtypes)} on cuda:{device}")
             arr[i] = nb_adamw_tensor(_ptr(grad), _ptr(param), _ptr(m), _ptr(v), _ptr(scales[0]), _ptr(scales[1]), _ptr(copy), n, int(group),
                                      0 if copy is None else _TORCH_DTYPES[str(copy.dtype)], _TORCH_DTYPES[str(grad.dtype)], bits)
-        self.count, self.device = len(items), device
+        self.count, self.device, self.tensors = len(items), device, items  # (the plan holds their addresses: they live as long)
         self._hyper = self._scaler = (None, None)  # (values, structure) of the last step: they seldom change
         self.handle = c_void_p()
         _check(load().nb_adamw_plan_create(arr, self.count, device, byref(self.handle)))
@@ -554,6 +554,7 @@ class AdamWPlan:
         if self.handle:
             load().nb_adamw_plan_destroy(self.handle)
             self.handle = c_void_p()
+        self.tensors = ()
 
     def __del__(self):
         try:

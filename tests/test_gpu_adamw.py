@@ -361,3 +361,31 @@ def test_a_nan_gradient_makes_the_clipped_step_nan(bits):
             assert st.t[0]["p"].isnan().all() and st.t[1]["p"].isnan().all()
         else:
             assert torch.equal(st.t[1]["p"], before)  # (group 1 has no decay)
+
+
+def test_a_plan_keeps_its_tensors():
+    """A plan holds addresses; moments that nothing else refers to stay allocated as long as it lives."""
+    import gc
+    import weakref
+
+    import torch
+
+    from paper_2609_10632_b200 import binding as nb
+
+    p, g = torch.zeros(1000, device="cuda"), torch.ones(1000, device="cuda")
+
+    def make():
+        m, v = torch.zeros(1000, device="cuda"), torch.zeros(1000, device="cuda")
+        return nb.AdamWPlan([(g, p, m, v, None, 0)]), weakref.ref(m), weakref.ref(v)
+
+    plan, m, v = make()
+    gc.collect()
+    assert m() is not None and v() is not None
+    ws = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda")
+    plan.upload(ws)
+    plan.step(ws, torch.zeros(1, dtype=torch.int64, device="cuda"), LR, WD, B1, B2, EPS, 0.0)
+    torch.cuda.synchronize()
+    assert torch.allclose(m(), torch.full_like(m(), 0.1))
+    plan.close()
+    gc.collect()
+    assert m() is None and v() is None
