@@ -23,8 +23,8 @@ struct Geom {
 // accumulators (see ChanAcc); each is zero whenever no kernel of the plan is running.
 enum { ST_ERR = 0, ST_WHERE = 1, ST_DETAIL = 2, ST_SAT = 3, ST_READERS_FWD = 8, ST_READERS_BWD = 10, ST_WORDS = 16 };
 // Sites that a give-up is reported from (ST_WHERE): 1-5 the roles of the implicit-GEMM kernel (A producer, accumulator
-// free, operands ready, accumulator ready, B producer), 11-15 the same roles of the weight-gradient kernel, 21-24 producer,
-// accumulator free, operands ready and accumulator ready of the MLP products.
+// free, operands ready, accumulator ready, B producer), 11-15 the same roles of the weight-gradient kernel, 21-25 producer,
+// accumulator free, operands ready, accumulator ready and epilogue input ready of the MLP products.
 
 // Every wait on an mbarrier (a CTA's own, on which in a CTA pair its peer arrives too) is bounded: about two seconds.  Nothing
 // else is waited for in a loop: no kernel waits for another kernel's flag, nor for a CTA outside its cluster.  The CTAs of a

@@ -17,6 +17,12 @@ __device__ __forceinline__ uint64_t global_timer_ns() {
     return t;
 }
 
+// A wait has run out: recorded (the first one wins), and the CTA's other roles stop waiting.
+static __device__ __noinline__ void give_up(volatile int* abort_flag, int* status, int site) {
+    *abort_flag = 1;
+    report_timeout(status, site, (int)blockIdx.x);
+}
+
 // Bounded mbarrier wait: gives up after `limit_ns` (or as soon as another role has given up), records the site.
 static __device__ __noinline__ bool wait_bar(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status, int site, uint64_t limit_ns = kWaitLimitNs) {
     uint64_t t0 = 0;
@@ -28,8 +34,7 @@ static __device__ __noinline__ bool wait_bar(uint64_t* bar, uint32_t parity, vol
             if (t0 == 0) {
                 t0 = now;
             } else if (now - t0 > limit_ns) {
-                *abort_flag = 1;
-                report_timeout(status, site, (int)blockIdx.x);
+                give_up(abort_flag, status, site);
                 return false;
             }
         }

@@ -493,6 +493,7 @@ template <typename T, int KIND, bool CG2, int NP> __global__ void __launch_bound
                         bool there = false;
                         for (int j = 0; j < 400000 && !(there = ptx::mbar_try_wait(my_in + buf, (in_ph >> buf) & 1u)); ++j) {
                         }
+                        if (!there) give_up(abort_flag, p.status, 25);
                         ok = __all_sync(0xffffffffu, ok && there) != 0;
                         in_ph ^= 1u << buf;
                         if (!ok && k < 2) {  // (those requested so far)

@@ -84,3 +84,20 @@ def test_plan_create_without_a_device_fails_loudly(lib):
     with pytest.raises(nb.NbError) as e:
         nb.LinearPlan(64, 64, nb.NB_DTYPE_BF16)
     assert e.value.status == nb.NB_ERR_CUDA
+
+
+def test_every_wait_of_the_tensor_core_products_reports_when_it_gives_up():
+    """Read from the source, since no call may make a wait run out: each role waits at a site of its own that the list in common.cuh counts,
+    through wait_bar / wait_bar_fast or a bounded loop with give_up behind it; a bare loop over mbar_try_wait only follows a wait
+    that has given up (for what is still in flight), or waits for the MMAs issued so far before TMEM is released."""
+    import os
+    import re
+
+    csrc = os.path.join(os.path.dirname(os.path.abspath(nb.__file__)), "csrc")
+    lines = open(os.path.join(csrc, "tc_linear.cuh")).read().split("\n")
+    sites = [int(m) for line in lines for m in re.findall(r"\b(?:wait_bar|wait_bar_fast|give_up)\([^;]*p\.status, (\d+)\)", line)]
+    assert sorted(sites) == [21, 22, 23, 24, 25]
+    assert "21-25" in open(os.path.join(csrc, "common.cuh")).read()
+    for i, line in enumerate(lines):
+        if "mbar_try_wait" in line:
+            assert "drain" in line or "give_up(" in lines[i + 2] or any("if (!ok)" in before for before in lines[i - 6 : i]), (i + 1, line)
