@@ -10,7 +10,7 @@
  *
  * x, y, g, add, dx are of `dtype` (nb_dtype), rows x c, the channels contiguous, rows ld_* elements apart (0 = dense, else >= c:
  * a channel slice of a wider tensor); gamma, beta, mean, rstd, dgamma, dbeta are fp32 and dense.  All statistics and sums are
- * formed in fp32 or more from the values as they are stored and each result is rounded once (fp16 saturates at +-65504, a NaN stays one).
+ * formed in fp32 or more from the values as they are stored and each result is rounded once (fp16 saturates at +-65504, uncounted; a NaN stays one).
  * Any c from 1 to 2^24 and any element-aligned pointer is taken; rows of whole 16-byte vectors (pointers, c and pitches) are the fast
  * ones.  y may be x, and dx may be g or add, where pointer and pitch are the same; otherwise outputs overlap nothing.
  * Sums are taken in a fixed order: results are bitwise reproducible on a given device.

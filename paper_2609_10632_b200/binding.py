@@ -583,7 +583,9 @@ class LinearPlan:
         return {"fwd": p3[0], "data": p3[1], "weight": p3[2]}
 
     def poll(self, stream=None):
+        """Waits for the stream and raises where a kernel gave up a wait; returns a note where fp16 results saturated, else ""."""
         _check(load().nb_linear_poll_status(self.handle, _stream_on(stream, self.device)))
+        return nb_last_error()
 
     def close(self):
         if self.handle:

@@ -1,6 +1,8 @@
 // Matrix products of MLP layers on the CUDA cores, their activations, and the sums of split products (see include/nb_linear.h
 // for the arithmetic; the tensor-core kernel is tc_linear.cuh).
 #pragma once
+#include <type_traits>
+
 #include "../../include/nb_linear.h"
 #include "common.cuh"
 
@@ -105,7 +107,17 @@ struct LinArgs {
     void* z;                // [M][N]
     void* out;              // LIN_WEIGHT: fp32
     long long ld_out;
+    int* status;            // of the plan
 };
+
+// One result, rounded; fp16: a saturated one is counted.
+template <typename T> __device__ __forceinline__ T lin_rounded(const LinArgs& P, float v) {
+    const T r = from_f32<T>(v);
+    if constexpr (std::is_same<T, __half>::value) {
+        if ((__half_as_ushort(r) & 0x7fffu) >= 0x7bffu) atomicAdd(P.status + ST_SAT, 1);
+    }
+    return r;
+}
 
 template <typename T, int KIND> __device__ __forceinline__ void lin_store(const LinArgs& P, long long m, long long n, float v) {
     if (KIND == LIN_WEIGHT) {
@@ -114,14 +126,14 @@ template <typename T, int KIND> __device__ __forceinline__ void lin_store(const 
     }
     if (KIND == LIN_FWD) {
         if (P.bias) v += P.bias[n];
-        if (P.z) static_cast<T*>(P.z)[m * P.N + n] = from_f32<T>(v);
+        if (P.z) static_cast<T*>(P.z)[m * P.N + n] = lin_rounded<T>(P, v);
         v = lin_act(v, P.act);
         if (P.add) v += to_f32<T>(static_cast<const T*>(P.add)[m * P.ld_add + n]);
     } else {
         if (P.add) v += to_f32<T>(static_cast<const T*>(P.add)[m * P.ld_add + n]);
         if (P.zin) v *= lin_act_grad(to_f32<T>(static_cast<const T*>(P.zin)[m * P.N + n]), P.act);
     }
-    static_cast<T*>(P.out)[m * P.ld_out + n] = from_f32<T>(v);
+    static_cast<T*>(P.out)[m * P.ld_out + n] = lin_rounded<T>(P, v);
 }
 
 // Bound: FMA issue.  A block of 256 threads has a [TILE x TILE] tile: 128 (a thread [8 x 8]: four 16-byte shared loads for 64 products) where

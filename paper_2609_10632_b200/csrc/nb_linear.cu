@@ -435,11 +435,12 @@ nb_status nb_linear_poll_status(nb_linear_plan p, void* stream) {
     int host[ST_WORDS] = {0};
     NB_CUDA_CHECK(cudaMemcpyAsync(host, p->status, sizeof host, cudaMemcpyDeviceToHost, st));
     NB_CUDA_CHECK(cudaStreamSynchronize(st));
-    if (host[ST_ERR]) {
+    if (host[ST_ERR] || host[ST_SAT]) {
         NB_CUDA_CHECK(cudaMemsetAsync(p->status, 0, sizeof host, st));
         NB_CUDA_CHECK(cudaStreamSynchronize(st));
-        return fail((nb_status)host[ST_ERR], "a kernel gave up a bounded wait (site %d, block %d)", host[ST_WHERE], host[ST_DETAIL]);
     }
+    if (host[ST_ERR]) return fail((nb_status)host[ST_ERR], "a kernel gave up a bounded wait (site %d, block %d)", host[ST_WHERE], host[ST_DETAIL]);
+    if (host[ST_SAT]) fail(NB_OK, "%d fp16 stores of the products' results saturated", host[ST_SAT]);
     return NB_OK;
 }
 
@@ -464,7 +465,7 @@ nb_status nb_linear_fwd(nb_linear_plan p, int64_t rows, const void* x, int64_t l
     memset(&A, 0, sizeof A);
     A.a = x; A.lda = ld_x; A.b = w; A.ldb = ci;
     A.M = rows; A.N = co; A.K = ci;
-    A.bias = bias; A.act = act; A.add = res; A.ld_add = ld_res; A.z = z; A.out = out; A.ld_out = ld_out;
+    A.status = p->status; A.bias = bias; A.act = act; A.add = res; A.ld_add = ld_res; A.z = z; A.out = out; A.ld_out = ld_out;
     if (few_rows(p, rows) && whole16(x, ld_x, es)) {
         if (p->d.dtype == NB_DTYPE_F32) return run_rows<float>(p, A, (int)rows, st);
         if (p->d.dtype == NB_DTYPE_BF16) return run_rows<__nv_bfloat16>(p, A, (int)rows, st);
@@ -522,7 +523,7 @@ nb_status nb_linear_bwd_data(nb_linear_plan p, int64_t rows, const void* dy, int
     memset(&A, 0, sizeof A);
     A.a = dy; A.lda = ld_dy; A.b = w; A.ldb = ci;
     A.M = rows; A.N = ci; A.K = co;
-    A.act = act_in; A.zin = z_in; A.add = add; A.ld_add = ld_add; A.out = dx; A.ld_out = ld_dx;
+    A.status = p->status; A.act = act_in; A.zin = z_in; A.add = add; A.ld_add = ld_add; A.out = dx; A.ld_out = ld_dx;
     return run_simt_any<LIN_DATA>(p, A, vec4(dy, ld_dy, co, es) && vec4(w, ci, ci, es), workspace, st);
 }
 

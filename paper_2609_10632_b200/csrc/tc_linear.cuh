@@ -66,11 +66,14 @@ template <typename T, int KIND, int NP> struct TlPass {
     static __device__ __forceinline__ uint4* piece(uint8_t* stg, int lane, int j) {
         return reinterpret_cast<uint4*>(stg + lane * (NP * 2) + (NP == 64 ? (j ^ (lane & 7)) : (j ^ ((lane >> 1) & 3))) * 16);
     }
-    static __device__ __forceinline__ void stage(uint8_t* stg, int lane, const float2 (&v)[NP / 2]) {
+    // (fp16: a lane whose part of a row of the matrix holds a saturated value counts it)
+    static __device__ __forceinline__ void stage(const TcLinParams& p, uint8_t* stg, int lane, int row0, const float2 (&v)[NP / 2]) {
+        int sat = 0;
 #pragma unroll
         for (int j = 0; j < NP / 8; ++j)
-            *piece(stg, lane, j) = make_uint4(pack2<T>(v[4 * j].x, v[4 * j].y, nullptr), pack2<T>(v[4 * j + 1].x, v[4 * j + 1].y, nullptr),
-                                              pack2<T>(v[4 * j + 2].x, v[4 * j + 2].y, nullptr), pack2<T>(v[4 * j + 3].x, v[4 * j + 3].y, nullptr));
+            *piece(stg, lane, j) = make_uint4(pack2<T>(v[4 * j].x, v[4 * j].y, &sat), pack2<T>(v[4 * j + 1].x, v[4 * j + 1].y, &sat),
+                                              pack2<T>(v[4 * j + 2].x, v[4 * j + 2].y, &sat), pack2<T>(v[4 * j + 3].x, v[4 * j + 3].y, &sat));
+        if ((sat & (int)0x80008000u) && row0 + lane < p.M) atomicAdd(p.status + ST_SAT, 1);
     }
     // this row's pieces of a matrix [M][N], straight from memory
     static __device__ __forceinline__ void direct(const TcLinParams& p, uint4 (&d)[NP / 8], const void* base, long long ld, long long row, int col) {
@@ -115,7 +118,7 @@ template <typename T, int KIND, int NP> struct TlPass {
             }
             if (p.want_z) {
                 uint8_t* zs = other();
-                stage(zs, lane, v);
+                stage(p, zs, lane, row0, v);
                 send(&p.tmZ, zs, lane, col, row0);
             }
             if (p.act == NB_ACT_GELU) {
@@ -150,7 +153,7 @@ template <typename T, int KIND, int NP> struct TlPass {
             if (lane == 0) ptx::tma_store_wait_read<1>();
             __syncwarp();
         }
-        stage(stg, lane, v);
+        stage(p, stg, lane, row0, v);
         send(&p.tmOut, stg, lane, col, row0);
         __syncwarp();  // (the next accumulator load wants the whole warp)
     }

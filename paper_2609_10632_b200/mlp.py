@@ -55,6 +55,11 @@ class MlpBlock:
         with torch.cuda.device(self.dev):
             self._backward(stream)
 
+    def poll(self, stream=None):
+        """Waits for the stream and raises where a product gave up a wait; returns a note where fp16 results of one saturated, else ""."""
+        notes = [(name, plan.poll(stream)) for name, plan in (("up", self.up), ("down", self.down))]
+        return "; ".join(f"{name}: {note}" for name, note in notes if note)
+
     def _forward(self, stream):
         p = self.param
         nb.nb_layer_norm_fwd(self.dtype, self.rows, self.c, self.x, p["gamma"], p["beta"], self.eps, self.h, self.mean, self.rstd, stream=stream)
