@@ -9,7 +9,8 @@
  * with act one of nb_act: none, SiLU z/(1+e^-z), GELU z*Phi(z) (Phi the normal distribution function, not its tanh approximation).
  * A layer whose own activation is not followed by another layer of this kind takes nb_act_bwd for the gradient of its z.
  *
- * x, w, res, z, out, dy, add, z_in, dx are of the plan's dtype; bias, dw, dbias are fp32.  Products are accumulated in fp32, the
+ * x, w, res, z, out, dy, add, z_in, dx are of the plan's dtype; bias, dw, dbias are fp32.  Products are accumulated in fp32 (on the
+ * tensor cores, which cut off low bits, no further than a fifth of half a step of the type: longer sums leave them in between), the
  * epilogue works on the fp32 sums and rounds once (z and out each once, from the same sum); fp16 stores saturate at +-65504 (a NaN stays one).
  *   NB_DTYPE_BF16 / NB_DTYPE_F16: tcgen05 tensor cores where c_in and c_out are multiples of 8 and pitches and pointers whole
  *     16-byte vectors, and on padded copies (in the workspace) of layers with other channel counts from 2^27 products on

@@ -44,10 +44,13 @@ double stage_cycles(bool cg2, int bn, bool weight) {
 // products or its epilogue, whichever is longer; the epilogue has a part of its own (handing the accumulators over, twice as long
 // between the CTAs of a pair) and `per_col` cycles for each column.  25600 x 384 -> 1536 with GELU and z: 53 and 57 us on pairs with 256 and 192
 // columns, 48 and 49 on single CTAs; the data gradient through GELU 72, 67 and 61, 58; 25600 x 1536 -> 384 34, 29 and 36, 34.
-TlCfg choose_rows(long long M, long long N, long long K, int sms, double per_col) {
+// Products of more than `chunk` k-blocks take the kernel whose sums leave the tensor cores in between, on tiles of 128 columns: what that
+// exactness costs is 4096 x 32768 -> 1024 in fp16 203 -> 243 us, 2048 x 151936 -> 2048 in bf16 908 -> 1036.
+TlCfg choose_rows(long long M, long long N, long long K, int sms, double per_col, int chunk) {
     TlCfg best;
     for (int cg2 = 1; cg2 >= 0; --cg2)
         for (int bn = 256; bn >= 64; bn -= 64) {
+            if (K > (long long)chunk * TL_KC && bn != 128) continue;
             TlCfg c;
             c.cg2 = cg2 != 0;
             c.bn = bn;
@@ -167,6 +170,8 @@ size_t workspace_for(const nb_linear_plan_s* p, long long rows) {
     return b;
 }
 
+// k-blocks that a 16-bit result's sum may stay in the tensor cores.
+int long_sum(const nb_linear_plan_s* p) { return p->d.dtype == NB_DTYPE_F16 ? TL_LONG_F16 : TL_LONG_BF16; }
 // Columns of an epilogue pass: a warp has half of a tile's.
 int pass_cols(const TlCfg& c) { return c.bn % 128 == 0 ? 64 : 32; }
 
@@ -186,20 +191,21 @@ bool encode2(CUtensorMap* m, int32_t dtype, const void* base, long long rows, lo
     return encode(m, dtype, base, 2, dims, strides, box, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, true);
 }
 
-template <typename T, int KIND, bool CG2, int NP> nb_status launch_tc(const nb_linear_plan_s* plan, const TcLinParams& P, unsigned grid, size_t smem, cudaStream_t st) {
+template <typename T, int KIND, bool CG2, int NP, bool LONG> nb_status launch_tc(const nb_linear_plan_s* plan, const TcLinParams& P, unsigned grid, size_t smem, cudaStream_t st) {
     static std::atomic<unsigned long long> attr_set{0};  // one bit per device ordinal
     const unsigned long long bit = 1ull << (plan->device & 63);
     if (!(attr_set.load(std::memory_order_acquire) & bit)) {
-        NB_CUDA_CHECK(cudaFuncSetAttribute(tc_linear_kernel<T, KIND, CG2, NP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tcdetail::kMaxSmem));
+        NB_CUDA_CHECK(cudaFuncSetAttribute(tc_linear_kernel<T, KIND, CG2, NP, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tcdetail::kMaxSmem));
         attr_set.fetch_or(bit, std::memory_order_release);
     }
-    launch_k(tc_linear_kernel<T, KIND, CG2, NP>, dim3(grid), dim3(TL_THREADS), smem, st, CG2 ? 2 : 1, P);
+    launch_k(tc_linear_kernel<T, KIND, CG2, NP, LONG>, dim3(grid), dim3(TL_THREADS), smem, st, CG2 ? 2 : 1, P);
     return launch_ok("tc_linear");
 }
 
 template <int KIND> nb_status run_tc(const nb_linear_plan_s* plan, const TlCfg& c, TcLinParams& P, cudaStream_t st) {
     const bool f16 = plan->d.dtype == NB_DTYPE_F16;
     P.kblocks = c.kblocks;
+    P.chunk = long_sum(plan);
     P.BN = c.bn;
     P.m_tiles = c.m_tiles;
     P.n_tiles = c.n_tiles;
@@ -221,11 +227,12 @@ template <int KIND> nb_status run_tc(const nb_linear_plan_s* plan, const TlCfg& 
     if (tiles > 0x3fffffffLL) return fail(NB_ERR_UNSUPPORTED, "too many tiles");
     const long long workers = c.cg2 ? plan->sms / 2 : plan->sms;
     const unsigned grid = (unsigned)((KIND == LIN_WEIGHT ? tiles : std::min(tiles, workers)) * (c.cg2 ? 2 : 1));
-#define NB_TL(T, NP) (c.cg2 ? launch_tc<T, KIND, true, NP>(plan, P, grid, smem, st) : launch_tc<T, KIND, false, NP>(plan, P, grid, smem, st))
+#define NB_TL(T, NP, LONG) (c.cg2 ? launch_tc<T, KIND, true, NP, LONG>(plan, P, grid, smem, st) : launch_tc<T, KIND, false, NP, LONG>(plan, P, grid, smem, st))
     if constexpr (KIND != LIN_WEIGHT) {
-        if (pass_cols(c) == 64) return f16 ? NB_TL(__half, 64) : NB_TL(__nv_bfloat16, 64);
+        if (c.kblocks > P.chunk) return f16 ? NB_TL(__half, 64, true) : NB_TL(__nv_bfloat16, 64, true);
+        if (pass_cols(c) == 64) return f16 ? NB_TL(__half, 64, false) : NB_TL(__nv_bfloat16, 64, false);
     }
-    return f16 ? NB_TL(__half, 32) : NB_TL(__nv_bfloat16, 32);
+    return f16 ? NB_TL(__half, 32, false) : NB_TL(__nv_bfloat16, 32, false);
 #undef NB_TL
 }
 
@@ -291,7 +298,7 @@ template <typename T> nb_status run_rows(const nb_linear_plan_s* plan, LinArgs& 
 // on operands whose rows are whole vectors; N and K may be padded counts (w has c_out rows all the same)
 nb_status tc_fwd(const nb_linear_plan_s* p, long long rows, const void* x, long long ld_x, const void* w, const float* bias, int act, const void* res, long long ld_res, void* z,
                  void* out, long long ld_out, int ci, int co, cudaStream_t st) {
-    const TlCfg c = choose_rows(rows, co, ci, p->sms, 15.0 + (bias ? 3.0 : 0.0) + (act == NB_ACT_GELU ? 8.0 : act ? 4.5 : 0.0) + (z ? 4.0 : 0.0) + (res ? 10.0 : 0.0));
+    const TlCfg c = choose_rows(rows, co, ci, p->sms, 15.0 + (bias ? 3.0 : 0.0) + (act == NB_ACT_GELU ? 8.0 : act ? 4.5 : 0.0) + (z ? 4.0 : 0.0) + (res ? 10.0 : 0.0), long_sum(p));
     TcLinParams P;
     memset(&P, 0, sizeof P);
     P.M = (int)rows; P.N = co; P.n_bias = p->d.c_out;
@@ -305,7 +312,7 @@ nb_status tc_fwd(const nb_linear_plan_s* p, long long rows, const void* x, long 
 }
 nb_status tc_data(const nb_linear_plan_s* p, long long rows, const void* dy, long long ld_dy, const void* w, const void* z_in, int act_in, const void* add, long long ld_add, void* dx,
                   long long ld_dx, int ci, int co, cudaStream_t st) {
-    const TlCfg c = choose_rows(rows, ci, co, p->sms, 15.0 + (act_in == NB_ACT_GELU ? 24.0 : z_in ? 14.0 : 0.0) + (add ? 10.0 : 0.0));
+    const TlCfg c = choose_rows(rows, ci, co, p->sms, 15.0 + (act_in == NB_ACT_GELU ? 24.0 : z_in ? 14.0 : 0.0) + (add ? 10.0 : 0.0), long_sum(p));
     TcLinParams P;
     memset(&P, 0, sizeof P);
     P.M = (int)rows; P.N = ci;

@@ -20,11 +20,14 @@ constexpr uint32_t TL_BLK = 64 * 128;         // an MN-major block: 64 m (or n) 
 constexpr uint32_t TL_A_BYTES = 128 * 128;    // A rows of a CTA by 64 k
 constexpr int TL_STG = 4096;     // staging buffer of an epilogue warp: 32 rows of 128 bytes; it has two
 constexpr int TL_CHUNK = 16;                    // k-blocks after which a weight gradient's sums leave the tensor cores
+// ... of a forward product or data gradient: 1024 additions are off by 9e-5 at most, 8192 by 7e-4, both 0.18 of half a step of the type.
+constexpr int TL_LONG_F16 = 256, TL_LONG_BF16 = 2048;
 constexpr uint32_t TL_ONES_BYTES = 4096;
 
 struct TcLinParams {
     CUtensorMap tmA, tmB, tmOut, tmZ, tmIn;  // tmIn: the residual (forward), z_in (data gradient)
     int M, N, kblocks;  // k-blocks of TL_KC
+    int chunk;          // LONG: k-blocks after which the sums leave the tensor cores
     int n_bias;         // columns that have a bias (N may be padded)
     int BN, m_tiles, n_tiles, group_m;
     int stages, acc_stride;
@@ -62,7 +65,7 @@ template <typename T> __device__ __forceinline__ float2 tl_pair(const uint4& v, 
 // One pass of the epilogue by a warp: NP (64 or 32) accumulator columns of its 32 rows become results.  A lane has one row's.  They go
 // through one of the warp's staging buffers (rows of 2*NP bytes in the swizzle of that width) and leave as a TMA store; a residual or
 // z_in has come into the same buffer by a TMA load.  Both run beside the arithmetic.
-template <typename T, int KIND, int NP> struct TlPass {
+template <typename T, int KIND, int NP, bool LONG> struct TlPass {
     static __device__ __forceinline__ uint4* piece(uint8_t* stg, int lane, int j) {
         return reinterpret_cast<uint4*>(stg + lane * (NP * 2) + (NP == 64 ? (j ^ (lane & 7)) : (j ^ ((lane >> 1) & 3))) * 16);
     }
@@ -89,9 +92,9 @@ template <typename T, int KIND, int NP> struct TlPass {
             ptx::tma_store_commit();
         }
     }
-    // `in_here`: the pass's input lies in buffer `stg`; `other` gives z a buffer
+    // `in_here`: the pass's input lies in buffer `stg`; `other` gives z a buffer; `sum`: LONG, what earlier chunks of k have given
     template <class Release, class Other>
-    static __device__ __forceinline__ void run(const TcLinParams& p, uint32_t taddr, int lane, int row0, int col, const float* bias, uint8_t* stg, bool in_here, Release release, Other other) {
+    static __device__ __forceinline__ void run(const TcLinParams& p, uint32_t taddr, int lane, int row0, int col, const float* bias, uint8_t* stg, bool in_here, const float2* sum, Release release, Other other) {
         uint32_t r[NP];
 #pragma unroll
         for (int h = 0; h < NP / 32; ++h) ptx::tmem_ld_32x32b_x32(taddr + 32u * h, r + 32 * h);
@@ -106,7 +109,10 @@ template <typename T, int KIND, int NP> struct TlPass {
         release();
         float2 v[NP / 2];
 #pragma unroll
-        for (int j = 0; j < NP / 2; ++j) v[j] = make_float2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+        for (int j = 0; j < NP / 2; ++j) {
+            v[j] = make_float2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+            if (LONG) v[j] = add2(sum[j], v[j]);
+        }
         if (KIND == LIN_FWD) {
             if (p.bias) {
 #pragma unroll
@@ -159,7 +165,7 @@ template <typename T, int KIND, int NP> struct TlPass {
     }
 };
 
-template <typename T, int KIND, bool CG2, int NP> __global__ void __launch_bounds__(TL_THREADS, 1) tc_linear_kernel(const __grid_constant__ TcLinParams p) {
+template <typename T, int KIND, bool CG2, int NP, bool LONG> __global__ void __launch_bounds__(TL_THREADS, 1) tc_linear_kernel(const __grid_constant__ TcLinParams p) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* sA = smem;
@@ -229,8 +235,9 @@ template <typename T, int KIND, bool CG2, int NP> __global__ void __launch_bound
     const uint32_t tmem_base = *tmem_slot;
     // The tensor cores add to their accumulator with truncation: 1024 additions (16384 rows) left a weight gradient 1.9e-5 off, relative
     // to its norm, always towards zero.  So a weight gradient's sums leave them every TL_CHUNK k-blocks (64 additions) and are added in
-    // fp32 registers, beside the next chunk's products in the other accumulator set; 1e-6 is left.  (Results in 16 bits do not see it.)
-    const int chunk = KIND == LIN_WEIGHT ? TL_CHUNK : p.kblocks;
+    // fp32 registers, beside the next chunk's products in the other accumulator set; 1e-6 is left.  Sums of positive terms lose most, 8.5e-8
+    // of the sum at every addition; a 16-bit result sees that when there are thousands, and LONG products do the same every p.chunk k-blocks.
+    const int chunk = KIND == LIN_WEIGHT ? TL_CHUNK : LONG ? p.chunk : p.kblocks;
     // a work item: a tile and, for the weight gradient, a slice of the rows
     auto item = [&](int i, int& mt, int& nt, int& split, int& kb0, int& kb1) {
         split = 0;
@@ -486,7 +493,27 @@ template <typename T, int KIND, bool CG2, int NP> __global__ void __launch_bound
                         request(buf ^ 1, 1);
                     }
                 }
-                bool ok = wait_acc();
+                bool ok = true;
+                float2 sum[LONG ? NP / 2 : 1];
+                if constexpr (LONG) {  // (tiles of 2 * NP columns: a warp has one pass)
+#pragma unroll
+                    for (int j = 0; j < NP / 2; ++j) sum[j] = make_float2(0.f, 0.f);
+                    for (int c0 = kb0; c0 + chunk < kb1; c0 += chunk) {
+                        ok = wait_acc();
+                        if (!ok) break;
+#pragma unroll
+                        for (int h = 0; h < NP / 32; ++h) {
+                            uint32_t r[32];
+                            ptx::tmem_ld_32x32b_x32(lanes + (uint32_t)(acc * p.acc_stride + c_lo + 32 * h), r);
+                            ptx::tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) sum[16 * h + j] = add2(sum[16 * h + j], make_float2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])));
+                        }
+                        release_acc();
+                        next_acc();
+                    }
+                }
+                if (ok) ok = wait_acc();
                 const uint32_t taddr = lanes + (uint32_t)(acc * p.acc_stride + c_lo);
                 if (ok && passes == 0) release_acc();
                 for (int k = 0; k < passes; ++k) {
@@ -519,7 +546,7 @@ template <typename T, int KIND, bool CG2, int NP> __global__ void __launch_bound
                         if (lane == 0) ptx::tma_store_wait_read<1>();
                         __syncwarp();
                     }
-                    TlPass<T, KIND, NP>::run(p, taddr + (uint32_t)(k * NP), lane, row0, col0 + k * NP, my_bias + k * NP, p.want_z ? my_stg + (buf ^ 1) * TL_STG : b, in_tma, release, other);
+                    TlPass<T, KIND, NP, LONG>::run(p, taddr + (uint32_t)(k * NP), lane, row0, col0 + k * NP, my_bias + k * NP, p.want_z ? my_stg + (buf ^ 1) * TL_STG : b, in_tma, sum, release, other);
                     buf ^= 1;
                     if (in_tma && k + 2 < passes && lane == 0) {
                         ptx::tma_store_wait_read<0>();

@@ -428,3 +428,53 @@ def test_refusals():
             call()
         assert e.value.status == status
     assert (out.buf == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype, rows, co, ci, kind", [
+    ("f16", 24, 72, 1 << 19, "fwd"), ("f16", 300, 136, 1 << 17, "fwd"), ("f16", 100, 64, 1 << 14, "fwd"), ("f16", 100, 64, (1 << 14) + 8, "fwd"), ("f16", 24, 1 << 19, 72, "data"),
+    ("f16", 300, 1 << 17, 200, "data"), ("bf16", 24, 72, 1 << 22, "fwd"), ("bf16", 33, 64, 1 << 17, "fwd"), ("bf16", 140, 1 << 20, 24, "data")])
+def test_products_of_very_many_terms(dtype, rows, co, ci, kind):
+    """Sums of positive terms, which the tensor cores cut off at every addition, stay within the roundings of their result and a quarter of
+    one more: (5/4) u|value|, u half a step of the type (the products' own header gives 0.18 for what stays in the tensor cores)."""
+    import torch
+
+    from paper_2609_10632_b200 import binding as nb
+
+    dt, code = _dt(torch, dtype)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    K = ci if kind == "fwd" else co
+    a = (0.5 + torch.rand(rows, K, device="cuda", generator=gen)).to(dt)
+    w = ((0.5 + torch.rand(co, ci, device="cuda", generator=gen)) * (1000.0 / K if dtype == "bf16" else 2.0**-6)).to(dt)
+    if dtype == "f16":
+        a *= 2.0**-6
+    plan = nb.LinearPlan(ci, co, code)
+    assert plan.paths(rows)[kind] == 1
+    ws = torch.empty(plan.workspace_bytes(rows), dtype=torch.uint8, device="cuda")
+    out = torch.full((rows + 1, co if kind == "fwd" else ci), 7.0, device="cuda").to(dt)
+    res = torch.zeros_like(out[:rows])
+    n = out.shape[1]
+    if kind == "fwd":
+        nb.nb_linear_fwd(plan, rows, a, w, torch.zeros(n, device="cuda"), 0, out, ws, res=res)
+    else:
+        nb.nb_linear_bwd_data(plan, rows, a, w, out, ws, add=res)
+    plan.poll()
+    want = torch.zeros(rows, n, dtype=torch.float64, device="cuda")
+    for k in range(0, K, 1 << 15):
+        s = slice(k, k + (1 << 15))
+        want += a[:, s].double() @ (w[:, s].double().T if kind == "fwd" else w[s].double())
+    off = ((out[:rows].double() - want).abs() / want).max().item()
+    assert off <= 1.25 * torch.finfo(dt).eps / 2, off / (torch.finfo(dt).eps / 2)
+    assert (out[rows] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype, k", [("f16", 16392), ("f16", 34000), ("bf16", 131080)])
+@pytest.mark.parametrize("rows, n", [(20, 8), (300, 200), (130, 400)])
+def test_epilogues_behind_very_many_terms(rows, n, dtype, k):
+    """One and several tiles of 128 columns, ragged ones, with everything that an epilogue can be given; a last chunk of one k-block."""
+    c = Case(rows, k, n, dtype, seed=n)
+    c.forward("gelu", res=True, keep_z=True)
+    c.forward("silu", res=True)
+    c = Case(rows, n, k, dtype, seed=n)
+    c.data("gelu", add=True)
+    c.data("silu")
+    c.data()
