@@ -334,10 +334,12 @@ __global__ void __launch_bounds__(L == 0 ? LN_BWD_MAX_BLOCK : LN_THREADS, L != 0
         if (r0 + step < P.rows) fetch(row + step);
         float2 sa = make_float2(0.f, 0.f), sx = sa;
 #pragma unroll
-        for (int k = 0; k < VPL; ++k)
+        for (int k = 0; k < VPL; ++k) {
+            const float rk = lane + k * W < P.nvec ? rstd : 0.f;
+            const float2 rs = make_float2(rk, V == 1 ? 0.f : rk);
 #pragma unroll
-            for (int j = 0; j < N; ++j) {  // (columns past the end have g = 0)
-                const float2 g = d[k].p[j], h = mul2(add2(xh[k].p[j], splat2(-mean)), splat2(rstd)), t = mul2(g, ga[k][j]);
+            for (int j = 0; j < N; ++j) {  // (columns past the end have g = 0, and xhat = 0 where mean * rstd would be inf)
+                const float2 g = d[k].p[j], h = mul2(add2(xh[k].p[j], splat2(-mean)), rs), t = mul2(g, ga[k][j]);
                 sa = add2(sa, t);
                 sx = fma2(t, h, sx);
                 if (SUMS) {
@@ -347,6 +349,7 @@ __global__ void __launch_bounds__(L == 0 ? LN_BWD_MAX_BLOCK : LN_THREADS, L != 0
                 d[k].p[j] = t;
                 xh[k].p[j] = h;
             }
+        }
         const float2 s = ln_sum2<L>(make_float2(sa.x + sa.y, sx.x + sx.y), red[turn]);
         turn ^= 1;
         const float2 r = splat2(rstd), a = splat2(-s.x * inv_c * rstd), b = splat2(-s.y * inv_c * rstd);

@@ -265,3 +265,19 @@ def test_offsets_past_32_bits():
     nb.nb_layer_norm_bwd(1, rows, c, y, x, None, mean, rstd, dx, ld_x=ld)
     nb.nb_layer_norm_bwd(1, rows, c, y, xc, None, mean, rstd, dx2)
     assert torch.equal(dx, dx2)
+
+
+@pytest.mark.parametrize("c", [1, 31, 96, 97, 1000])
+def test_a_mean_that_times_rstd_overflows(c):
+    """Constant rows of 2^120 with rstd 2^12: x - mean is 0, so dx is rstd (g - mean of g).  Lanes without a channel form no 0 * inf."""
+    import torch
+
+    from paper_2609_10632_b200 import binding as nb
+
+    rows = 9
+    x, g, dx = torch.full((rows, c), 2.0**120, device="cuda"), torch.randn(rows, c, device="cuda"), torch.empty(rows, c, device="cuda")
+    mean, rstd = torch.full((rows,), 2.0**120, device="cuda"), torch.full((rows,), 2.0**12, device="cuda")
+    nb.nb_layer_norm_bwd(0, rows, c, g, x, None, mean, rstd, dx)
+    hg = g.double().cpu().numpy()
+    want = 4096.0 * (hg - hg.mean(1, keepdims=True))
+    _close("dx", dx, want, 2.0**-17 * 4096.0 * (np.abs(hg) + np.abs(hg).mean(1, keepdims=True)))
