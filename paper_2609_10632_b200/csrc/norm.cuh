@@ -90,6 +90,12 @@ template <int L> __device__ __forceinline__ float2 ln_sum2(float2 s, float2* red
     return s;
 }
 template <int L> __device__ __forceinline__ float ln_sum(float s, float2* red) { return ln_sum2<L>(make_float2(s, 0.f), red).x; }
+// s / c by the rounded reciprocal of c and one correction of the quotient: exact where the quotient is a number of fp32, so that a constant row's
+// mean is its constant (half a unit off, x - mean would be an error of 1000 * 2^-24 / sqrt(eps) in a row of 1000s).
+__device__ __forceinline__ float ln_mean(float s, float c, float inv_c) {
+    const float q = s * inv_c;
+    return fmaf(fmaf(-q, c, s), inv_c, q);
+}
 
 struct LnFwd {
     const void* x;
@@ -134,7 +140,7 @@ template <typename T, int V, int L, int VPL> __global__ void __launch_bounds__(L
 #pragma unroll
             for (int j = 0; j < N; ++j) s2 = add2(s2, f[k].p[j]);
         }
-        const float mean = ln_sum<L>(s2.x + s2.y, red[0]) * inv_c;
+        const float mean = ln_mean(ln_sum<L>(s2.x + s2.y, red[0]), (float)P.c, inv_c);
         s2 = make_float2(0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < VPL; ++k)
@@ -218,7 +224,7 @@ template <typename T> __global__ void __launch_bounds__(LN_TILE_THREADS) layer_n
             float s = 0.f;
 #pragma unroll 8
             for (int i = lane; i < P.c; i += 32) s += to_f32<T>(row[i]);
-            const float mean = ln_sum<32>(s, nullptr) * inv_c;
+            const float mean = ln_mean(ln_sum<32>(s, nullptr), (float)P.c, inv_c);
             s = 0.f;
 #pragma unroll 8
             for (int i = lane; i < P.c; i += 32) {
@@ -240,24 +246,41 @@ template <typename T> __global__ void __launch_bounds__(LN_TILE_THREADS) layer_n
     }
 }
 
+// The sum over a row of what `f` gives for its elements, by a whole block: eight at a time in fp32, those in fp64, since a thread may have
+// thousands (`red`: as in ln_sum2).
+template <typename F> __device__ __forceinline__ double ln_row_sum(int c, double* red, F f) {
+    double s = 0.0;
+    for (int i0 = threadIdx.x; i0 < c; i0 += 8 * blockDim.x) {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = i0 + u * (int)blockDim.x < c ? f(i0 + u * (int)blockDim.x) : 0.f;
+        s += (double)(((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
+    }
+    const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == 0) red[threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = lane < warps ? red[lane] : 0.0;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    return s;
+}
+
 // Any channel count: a block a row, the row read three times (the second and third time from the caches).
 template <typename T> __global__ void __launch_bounds__(LN_MAX_BLOCK) layer_norm_fwd_loop_kernel(LnFwd P) {
     pdl_launch_dependents();
     pdl_wait();
-    __shared__ float2 red[2][32];
-    const float inv_c = 1.f / (float)P.c;
+    __shared__ double red[2][32];
     for (long long row = blockIdx.x; row < P.rows; row += gridDim.x) {
         const T* x = static_cast<const T*>(P.x) + row * P.ld_x;
         T* y = static_cast<T*>(P.y) + row * P.ld_y;
-        float s = 0.f;
-        for (int i = threadIdx.x; i < P.c; i += blockDim.x) s += to_f32<T>(x[i]);
-        const float mean = ln_sum<0>(s, red[0]) * inv_c;
-        s = 0.f;
-        for (int i = threadIdx.x; i < P.c; i += blockDim.x) {
+        const float mean = (float)(ln_row_sum(P.c, red[0], [&](int i) { return to_f32<T>(x[i]); }) / P.c);
+        const float var = (float)(ln_row_sum(P.c, red[1], [&](int i) {
             const float d = to_f32<T>(x[i]) - mean;
-            s = fmaf(d, d, s);
-        }
-        const float rstd = 1.f / sqrtf(ln_sum<0>(s, red[1]) * inv_c + P.eps);
+            return d * d;
+        }) / P.c);
+        const float rstd = 1.f / sqrtf(var + P.eps);
         for (int i = threadIdx.x; i < P.c; i += blockDim.x)
             y[i] = from_f32<T>(fmaf((to_f32<T>(x[i]) - mean) * rstd, P.gamma ? P.gamma[i] : 1.f, P.beta ? P.beta[i] : 0.f));
         if (P.mean && threadIdx.x == 0) {

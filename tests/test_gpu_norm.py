@@ -281,3 +281,42 @@ def test_a_mean_that_times_rstd_overflows(c):
     hg = g.double().cpu().numpy()
     want = 4096.0 * (hg - hg.mean(1, keepdims=True))
     _close("dx", dx, want, 2.0**-17 * 4096.0 * (np.abs(hg) + np.abs(hg).mean(1, keepdims=True)))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("c", [24, 100, 1000, 1001, 1304, 5000, 20000, 100001, 1 << 20])
+def test_constant_rows_have_their_constant_as_mean(c, dtype):
+    """Constants whose sums are numbers of fp32 at every length, so that y is beta; and one whose sums are not: a lane adds up to 32 terms
+    one after the other and five levels follow, 37 roundings of 2^-24, which is below the 2^-18 of this file."""
+    import torch
+
+    from paper_2609_10632_b200 import binding as nb
+
+    dt, code, _ = _types(torch)[dtype]
+    x = torch.tensor([1000.0, -57.25, 3.0, 0.1], device="cuda").to(dt)[:, None].expand(4, c).contiguous()
+    y, mean, rstd, beta = torch.empty_like(x), torch.empty(4, device="cuda"), torch.empty(4, device="cuda"), torch.full((c,), 0.25, device="cuda")
+    nb.nb_layer_norm_fwd(code, 4, c, x, None, beta, EPS, y, mean, rstd)
+    assert torch.equal(mean[:3], x[:3, 0].float()) and (y[:3] == 0.25).all()
+    v = float(x[3, 0])
+    assert abs(float(mean[3]) - v) <= 2.0**-18 * v and ((y[3].double() - 0.25).abs() <= 2.0**-18 * v / EPS**0.5 + torch.finfo(dt).eps / 8).all()
+
+
+def test_rows_of_a_million_channels():
+    """Sums of a million terms of one sign and of both, forward and backward, to the roundings of fp32 values summed in fp64."""
+    import torch
+
+    from paper_2609_10632_b200 import binding as nb
+
+    c = (1 << 20) + 1
+    x = torch.rand(2, c, device="cuda") + torch.tensor([[3.0], [-0.5]], device="cuda")
+    g, ga = torch.rand(2, c, device="cuda") + 0.5, torch.rand(c, device="cuda") + 0.5
+    y, dx, mean, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(2, device="cuda"), torch.empty(2, device="cuda")
+    nb.nb_layer_norm_fwd(0, 2, c, x, ga, None, EPS, y, mean, rstd)
+    nb.nb_layer_norm_bwd(0, 2, c, g, x, ga, mean, rstd, dx)
+    f = lambda t: t.double().cpu().numpy()  # noqa: E731
+    want, wmean, wrstd = ora.layer_norm_fwd(f(x), f(ga), None, EPS)
+    _close("mean", mean, wmean, 2.0**-22 * np.abs(wmean) + 2.0**-22)  # (eight at a time in fp32: 2^-22 of their sum at most)
+    _close("rstd", rstd, wrstd, 2.0**-20 * wrstd)
+    _close("y", y, want, 2.0**-19 * (np.abs(want) + f(ga) * 4.0 * wrstd[:, None]))
+    wdx, _, _ = ora.layer_norm_bwd(f(g), f(x), f(ga), f(mean), f(rstd))
+    _close("dx", dx, wdx, 2.0**-19 * wrstd[:, None] * (2.25 + 2.25 + 2.0 * 2.25 * 2.0))
