@@ -308,14 +308,19 @@ template <typename T, int V> __global__ void __launch_bounds__(256) lin_colsum_k
     }
 }
 // dw (n1 elements, `s1` slices) and dbias (n2 elements, `s2` slices) from their slices, in one launch; a count of zero slices: nothing to add.
+// `add1`: what dw holds is added as well.
 static __global__ void __launch_bounds__(256) lin_weight_sums_kernel(const float* __restrict__ p1, int s1, long long n1, float* __restrict__ o1, const float* __restrict__ p2, int s2, int n2,
-                                                                     float* __restrict__ o2) {
+                                                                     float* __restrict__ o2, int add1) {
     pdl_launch_dependents();
     pdl_wait();
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x, step = (long long)gridDim.x * 256;
     if (s1 && (n1 & 3) == 0) {
         for (long long v = at; v < n1 / 4; v += step) {
             double s[4] = {0.0, 0.0, 0.0, 0.0};
+            if (add1) {
+                const float4 was = reinterpret_cast<const float4*>(o1)[v];
+                s[0] = was.x; s[1] = was.y; s[2] = was.z; s[3] = was.w;
+            }
             for (int z0 = 0; z0 < s1; z0 += 8) {  // eight slices in flight
                 float4 a[8];
 #pragma unroll
@@ -334,7 +339,7 @@ static __global__ void __launch_bounds__(256) lin_weight_sums_kernel(const float
         }
     } else if (s1) {
         for (long long i = at; i < n1; i += step) {
-            double s = 0.0;
+            double s = add1 ? (double)o1[i] : 0.0;
             for (int z = 0; z < s1; ++z) s += (double)p1[z * n1 + i];
             o1[i] = (float)s;
         }

@@ -121,6 +121,25 @@ SimtCfg simt_cfg(long long M, long long N, long long K, int sms, bool weight) {
     c.slices = (int)ceil_div(K, c.kslice);
     return c;
 }
+// Slices of a weight gradient on the CUDA cores that are in memory at once: at most 128 MB of them (or one).  The others follow, group by
+// group, added to dw.  All at once (4096 rows each) they were 236 MB for 409600 rows of 384 -> 1536 and 16 GB for a million of 4096 -> 4096,
+// in the workspace of tensor-core layers too, whose misaligned calls end up here.  Of the counts that fit, the one whose blocks leave the
+// fewest places empty (two blocks of 128-tiles an SM, four of 64): 409600 rows of 384 -> 1536 in fp32 8.8 ms as all at once, 11.1 in the
+// groups of 14 that 32 MB hold.
+int weight_group(const SimtCfg& c, long long M, long long N, int sms) {
+    const long long fit = std::max<long long>(1, (128ll << 20) / (M * N * 4)), places = (c.tile == 128 ? 2ll : 4ll) * sms;
+    if (c.slices <= fit) return c.slices;
+    int best = 1;
+    long long least = -1;
+    for (int g = (int)std::min<long long>(fit, c.slices); g >= 1; --g) {
+        const long long cost = c.slices / g * ceil_div(c.tiles * g, places) + ceil_div(c.tiles * (c.slices % g), places);
+        if (least < 0 || cost < least) {
+            least = cost;
+            best = g;
+        }
+    }
+    return best;
+}
 constexpr int COLSUM_PARTS = 128;
 // Ranges of rows of a column-sum pass over c columns, `v` a vector: about four blocks an SM.
 int colsum_parts(long long rows, long long c, int v, int sms) {
@@ -146,7 +165,8 @@ size_t simt_ws(const nb_linear_plan_s* p, long long rows, int kind) {
     const long long ci = p->d.c_in, co = p->d.c_out;
     const long long M = kind == LIN_WEIGHT ? co : rows, N = kind == LIN_FWD ? co : ci, K = kind == LIN_FWD ? ci : kind == LIN_DATA ? co : rows;
     const SimtCfg c = simt_cfg(M, N, K, p->sms, kind == LIN_WEIGHT);
-    size_t b = c.slices > 1 ? align_up((size_t)c.slices * M * N * 4, 256) : 0;
+    const int slices = kind == LIN_WEIGHT ? weight_group(c, M, N, p->sms) : c.slices;
+    size_t b = c.slices > 1 ? align_up((size_t)slices * M * N * 4, 256) : 0;
     if (kind == LIN_WEIGHT) b += align_up((size_t)COLSUM_PARTS * co * 4, 256);
     return b;
 }
@@ -237,8 +257,7 @@ template <int KIND> nb_status run_tc(const nb_linear_plan_s* plan, const TlCfg& 
 }
 
 // ---------------------------------------------------------------- CUDA cores: launch
-template <typename T, int KIND> nb_status run_simt(const nb_linear_plan_s* plan, LinArgs& P, bool vec, void* workspace, cudaStream_t st) {
-    const SimtCfg c = simt_cfg(P.M, P.N, P.K, plan->sms, KIND == LIN_WEIGHT);
+template <typename T, int KIND> nb_status run_simt(const nb_linear_plan_s* plan, LinArgs& P, const SimtCfg& c, bool vec, void* workspace, cudaStream_t st) {
     if (c.tiles > 0x7fffffffLL) return fail(NB_ERR_UNSUPPORTED, "too many tiles");
     P.kslice = c.kslice;
     P.slices = c.slices;
@@ -258,10 +277,10 @@ template <typename T, int KIND> nb_status run_simt(const nb_linear_plan_s* plan,
     }
     return NB_OK;
 }
-template <int KIND> nb_status run_simt_any(const nb_linear_plan_s* plan, LinArgs& P, bool vec, void* workspace, cudaStream_t st) {
-    if (plan->d.dtype == NB_DTYPE_F32) return run_simt<float, KIND>(plan, P, vec, workspace, st);
-    if (plan->d.dtype == NB_DTYPE_BF16) return run_simt<__nv_bfloat16, KIND>(plan, P, vec, workspace, st);
-    return run_simt<__half, KIND>(plan, P, vec, workspace, st);
+template <int KIND> nb_status run_simt_any(const nb_linear_plan_s* plan, LinArgs& P, const SimtCfg& c, bool vec, void* workspace, cudaStream_t st) {
+    if (plan->d.dtype == NB_DTYPE_F32) return run_simt<float, KIND>(plan, P, c, vec, workspace, st);
+    if (plan->d.dtype == NB_DTYPE_BF16) return run_simt<__nv_bfloat16, KIND>(plan, P, c, vec, workspace, st);
+    return run_simt<__half, KIND>(plan, P, c, vec, workspace, st);
 }
 
 // Sums of dy's columns over ranges of rows into `partial`; returns the number of ranges in *parts.
@@ -492,7 +511,7 @@ nb_status nb_linear_fwd(nb_linear_plan p, int64_t rows, const void* x, int64_t l
         if (z) NB_TRY(S.out(zs, rows, (int)co, z, co));
         return S.out(os, rows, (int)co, out, ld_out);
     }
-    return run_simt_any<LIN_FWD>(p, A, vec4(x, ld_x, ci, es) && vec4(w, ci, ci, es), workspace, st);
+    return run_simt_any<LIN_FWD>(p, A, simt_cfg(A.M, A.N, A.K, p->sms, false), vec4(x, ld_x, ci, es) && vec4(w, ci, ci, es), workspace, st);
 }
 
 nb_status nb_linear_bwd_data(nb_linear_plan p, int64_t rows, const void* dy, int64_t ld_dy, const void* w, const void* z_in, int32_t act_in, const void* add, int64_t ld_add,
@@ -531,7 +550,7 @@ nb_status nb_linear_bwd_data(nb_linear_plan p, int64_t rows, const void* dy, int
     A.a = dy; A.lda = ld_dy; A.b = w; A.ldb = ci;
     A.M = rows; A.N = ci; A.K = co;
     A.status = p->status; A.act = act_in; A.zin = z_in; A.add = add; A.ld_add = ld_add; A.out = dx; A.ld_out = ld_dx;
-    return run_simt_any<LIN_DATA>(p, A, vec4(dy, ld_dy, co, es) && vec4(w, ci, ci, es), workspace, st);
+    return run_simt_any<LIN_DATA>(p, A, simt_cfg(A.M, A.N, A.K, p->sms, false), vec4(dy, ld_dy, co, es) && vec4(w, ci, ci, es), workspace, st);
 }
 
 nb_status nb_linear_bwd_weight(nb_linear_plan p, int64_t rows, const void* x, int64_t ld_x, const void* dy, int64_t ld_dy, float* dw, float* dbias, void* workspace,
@@ -550,9 +569,9 @@ nb_status nb_linear_bwd_weight(nb_linear_plan p, int64_t rows, const void* x, in
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     const long long n1 = co * ci;
-    auto sums = [&](const float* p1, int s1, const float* p2, int s2) -> nb_status {
+    auto sums = [&](const float* p1, int s1, const float* p2, int s2, bool more = false) -> nb_status {
         const long long work = std::max(s1 ? ceil_div(n1, n1 % 4 ? 1 : 4) : 0LL, s2 ? (long long)co : 0LL);
-        launch_k(lin_weight_sums_kernel, dim3((unsigned)std::min<long long>(ceil_div(work, 256), p->sms * 8)), dim3(256), 0, st, 1, p1, s1, n1, dw, p2, s2, (int)co, dbias);
+        launch_k(lin_weight_sums_kernel, dim3((unsigned)std::min<long long>(ceil_div(work, 256), p->sms * 8)), dim3(256), 0, st, 1, p1, s1, n1, dw, p2, s2, (int)co, dbias, (int)more);
         return launch_ok("lin_weight_sums");
     };
     const bool whole = tc_layer(p) && whole16(x, ld_x, es) && whole16(dy, ld_dy, es), padded = !whole && tc_padded(p, rows);
@@ -599,13 +618,26 @@ nb_status nb_linear_bwd_weight(nb_linear_plan p, int64_t rows, const void* x, in
     memset(&A, 0, sizeof A);
     A.a = dy; A.lda = ld_dy; A.b = x; A.ldb = ld_x;
     A.M = co; A.N = ci; A.K = rows;
-    A.out = dw; A.ld_out = ci;
-    NB_TRY(run_simt_any<LIN_WEIGHT>(p, A, vec4(dy, ld_dy, co, es) && vec4(x, ld_x, ci, es), workspace, st));
-    const int slices = A.slices;
-    float* db = reinterpret_cast<float*>(ws + (slices > 1 ? align_up((size_t)slices * n1 * 4, 256) : 0));
+    A.ld_out = ci;
+    const SimtCfg c = simt_cfg(co, ci, rows, p->sms, true);
+    const bool vec = vec4(dy, ld_dy, co, es) && vec4(x, ld_x, ci, es);
+    const int group = weight_group(c, co, ci, p->sms);
+    float* part = static_cast<float*>(workspace);
+    float* db = reinterpret_cast<float*>(ws + (c.slices > 1 ? align_up((size_t)group * n1 * 4, 256) : 0));
     int parts = 0;
-    if (dbias) NB_TRY(run_colsum_any(p, dy, ld_dy, rows, db, &parts, st));
-    return slices > 1 || parts ? sums(static_cast<const float*>(workspace), slices > 1 ? slices : 0, db, parts) : NB_OK;
+    for (int s0 = 0; s0 < c.slices; s0 += group) {
+        SimtCfg g = c;
+        g.slices = std::min(group, c.slices - s0);
+        const long long k0 = s0 * c.kslice;
+        A.a = static_cast<const char*>(dy) + k0 * ld_dy * (long long)es;
+        A.b = static_cast<const char*>(x) + k0 * ld_x * (long long)es;
+        A.K = std::min<long long>(rows - k0, g.slices * c.kslice);
+        A.out = c.slices > 1 ? part : dw;  // (where a group is one slice; more go to `part` by themselves)
+        NB_TRY(run_simt_any<LIN_WEIGHT>(p, A, g, vec, workspace, st));
+        if (s0 == 0 && dbias) NB_TRY(run_colsum_any(p, dy, ld_dy, rows, db, &parts, st));
+        if (c.slices > 1 || parts) NB_TRY(sums(part, c.slices > 1 ? g.slices : 0, db, s0 ? 0 : parts, s0 > 0));
+    }
+    return NB_OK;
 }
 
 nb_status nb_act_bwd(int32_t dtype, int64_t n, int32_t act, const void* dy, const void* z, void* dz, void* stream) {

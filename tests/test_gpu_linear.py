@@ -478,3 +478,41 @@ def test_epilogues_behind_very_many_terms(rows, n, dtype, k):
     c.data("gelu", add=True)
     c.data("silu")
     c.data()
+
+
+@pytest.mark.parametrize("dtype, flags, rows, ci, co", [("f32", 0, 600000, 500, 700), ("bf16", 1, 33000, 2000, 2100), ("f32", 0, 9001, 4900, 3501), ("f16", 1, 900000, 300, 701)])
+def test_weight_gradients_whose_slices_come_in_groups(dtype, flags, rows, ci, co):
+    """More slices than are kept at once: two groups of many, groups of one.  E as above with 4096 terms a slice, and a rounding for each group."""
+    import torch
+
+    from paper_2609_10632_b200 import binding as nb
+
+    dt, code = _dt(torch, dtype)
+    plan = nb.LinearPlan(ci, co, code, flags=flags)
+    need = plan.workspace_bytes(rows)
+    assert need <= 130 << 20
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda").fill_(255)
+    x, dy = torch.randn(rows, ci, device="cuda").to(dt), torch.randn(rows, co, device="cuda").to(dt)
+    dw, db = torch.full((co * ci + 8,), 7.0, device="cuda"), torch.full((co + 8,), 7.0, device="cuda")
+    nb.nb_linear_bwd_weight(plan, rows, x, dy, dw, db, ws)
+    want, S = (torch.zeros(co, ci, dtype=torch.float64, device="cuda") for _ in range(2))
+    for k in range(0, rows, 1 << 16):
+        a, b = dy[k : k + (1 << 16)].double(), x[k : k + (1 << 16)].double()
+        want += a.T @ b
+        S += a.abs().T @ b.abs()
+    assert ((dw[: co * ci].view(co, ci).double() - want).abs() <= (4096 + 16) * 2.0**-24 * S + 8 * 2.0**-24 * S).all() and (dw[co * ci :] == 7.0).all()
+    assert ((db[:co].double() - dy.double().sum(0)).abs() <= (4096 + 24) * 2.0**-24 * dy.double().abs().sum(0)).all() and (db[co:] == 7.0).all()
+    first = dw.clone()
+    nb.nb_linear_bwd_weight(plan, rows, x, dy, dw, None, ws)
+    assert torch.equal(dw, first)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_workspace_does_not_grow_with_the_rows(dtype):
+    import torch
+
+    from paper_2609_10632_b200 import binding as nb
+
+    for ci, co in ((384, 1536), (4096, 4096), (4096, 16384)):
+        plan = nb.LinearPlan(ci, co, _dt(torch, dtype)[1])
+        assert all(plan.workspace_bytes(rows) <= ci * co * 4 + (160 << 20) for rows in (1, 100, 25600, 409600, 1 << 20, 1 << 24))
