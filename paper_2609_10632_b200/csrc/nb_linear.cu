@@ -42,11 +42,17 @@ double stage_cycles(bool cg2, int bn, bool weight) {
 
 // Tiles of a forward product or data gradient: the least time of the persistent loop over what the candidates give.  A tile takes its
 // products or its epilogue, whichever is longer; the epilogue has a part of its own (handing the accumulators over, twice as long
-// between the CTAs of a pair) and `per_col` cycles for each column.  25600 x 384 -> 1536 with GELU and z: 53 and 57 us on pairs with 256 and 192
-// columns, 48 and 49 on single CTAs; the data gradient through GELU 72, 67 and 61, 58; 25600 x 1536 -> 384 34, 29 and 36, 34.
+// between the CTAs of a pair) and `per_col` cycles for each column, `narrow` times as many in a forward product whose passes have 32
+// columns (tiles of 64 and 192), and `wait` for a residual's tile.  us, the same buffers again and again, tiles of 256, 192 and 128 columns:
+//   25600 x 384 -> 1536 with GELU and z   pairs 58.7, 65.0, 67.9   single CTAs 53.3, 58.6, 57.2
+//   the same with a residual, without z   pairs 68.1, 69.1, 77.8   single CTAs 60.8, 61.3, 70.7
+//   25600 x 384 -> 768 with GELU          pairs 30.8, 33.6, 35.8   single CTAs 29.2, 30.7, 28.7
+//   8192 x 1024 -> 4096 with GELU and z   pairs 63.1, 70.5, 72.0   single CTAs 67.1, 74.3, 75.3
+//   data gradient of 25600 x 1536 -> 384 through GELU   pairs 75.1, 68.1, 81.7   single CTAs 63.5, 59.0, 71.5
+//   25600 x 1536 -> 384 with bias         pairs 34.9, 29.5, 33.9   single CTAs 37.3, 34.1, 36.8
 // Products of more than `chunk` k-blocks take the kernel whose sums leave the tensor cores in between, on tiles of 128 columns: what that
 // exactness costs is 4096 x 32768 -> 1024 in fp16 203 -> 243 us, 2048 x 151936 -> 2048 in bf16 908 -> 1036.
-TlCfg choose_rows(long long M, long long N, long long K, int sms, double per_col, int chunk) {
+TlCfg choose_rows(long long M, long long N, long long K, int sms, double per_col, double narrow, double wait, int chunk) {
     TlCfg best;
     for (int cg2 = 1; cg2 >= 0; --cg2)
         for (int bn = 256; bn >= 64; bn -= 64) {
@@ -58,7 +64,7 @@ TlCfg choose_rows(long long M, long long N, long long K, int sms, double per_col
             c.n_tiles = (int)ceil_div(N, bn);
             c.kblocks = (int)ceil_div(K, TL_KC);
             const long long workers = cg2 ? sms / 2 : sms, tiles = (long long)c.m_tiles * c.n_tiles;
-            const double main = c.kblocks * stage_cycles(cg2, bn, false), epi = (cg2 ? 2800.0 : 1450.0) + bn * per_col;
+            const double main = c.kblocks * stage_cycles(cg2, bn, false), epi = (cg2 ? 2800.0 : 1450.0) + wait + bn * per_col * (bn % 128 ? narrow : 1.0);
             c.cost = (double)ceil_div(tiles, workers) * std::max(main, epi) + std::min(main, epi) + 1000.0;
             if (!best.bn || c.cost < best.cost) best = c;
         }
@@ -317,7 +323,8 @@ template <typename T> nb_status run_rows(const nb_linear_plan_s* plan, LinArgs& 
 // on operands whose rows are whole vectors; N and K may be padded counts (w has c_out rows all the same)
 nb_status tc_fwd(const nb_linear_plan_s* p, long long rows, const void* x, long long ld_x, const void* w, const float* bias, int act, const void* res, long long ld_res, void* z,
                  void* out, long long ld_out, int ci, int co, cudaStream_t st) {
-    const TlCfg c = choose_rows(rows, co, ci, p->sms, 15.0 + (bias ? 3.0 : 0.0) + (act == NB_ACT_GELU ? 8.0 : act ? 4.5 : 0.0) + (z ? 4.0 : 0.0) + (res ? 10.0 : 0.0), long_sum(p));
+    const TlCfg c = choose_rows(rows, co, ci, p->sms, 15.0 + (bias ? 3.0 : 0.0) + (act == NB_ACT_GELU ? 8.0 : act ? 4.5 : 0.0) + (z ? 4.0 : 0.0) + (res ? 4.0 : 0.0), 1.2, res ? 1000.0 : 0.0,
+                                long_sum(p));
     TcLinParams P;
     memset(&P, 0, sizeof P);
     P.M = (int)rows; P.N = co; P.n_bias = p->d.c_out;
@@ -331,7 +338,7 @@ nb_status tc_fwd(const nb_linear_plan_s* p, long long rows, const void* x, long 
 }
 nb_status tc_data(const nb_linear_plan_s* p, long long rows, const void* dy, long long ld_dy, const void* w, const void* z_in, int act_in, const void* add, long long ld_add, void* dx,
                   long long ld_dx, int ci, int co, cudaStream_t st) {
-    const TlCfg c = choose_rows(rows, ci, co, p->sms, 15.0 + (act_in == NB_ACT_GELU ? 24.0 : z_in ? 14.0 : 0.0) + (add ? 10.0 : 0.0), long_sum(p));
+    const TlCfg c = choose_rows(rows, ci, co, p->sms, 15.0 + (act_in == NB_ACT_GELU ? 24.0 : z_in ? 14.0 : 0.0) + (add ? 10.0 : 0.0), 1.0, 0.0, long_sum(p));
     TcLinParams P;
     memset(&P, 0, sizeof P);
     P.M = (int)rows; P.N = ci;

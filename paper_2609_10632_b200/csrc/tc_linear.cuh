@@ -379,9 +379,10 @@ template <typename T, int KIND, bool CG2, int NP, bool LONG> __global__ void __l
         }
     } else {
         // ------------------------------------------------------------------ epilogue: two teams of four warps, each half of a tile's columns
-        // Every warp goes its own way through its 32 rows.  25600 x 384 -> 1536 with GELU and z, 51 us on the tiles chosen now; on
-        // pairs of CTAs this form takes 56, lanes that store themselves (64-byte pieces of eight rows an instruction) 71, sixteen
-        // warps in teams with a buffer and barriers for each four 63 to 78, and their polling costs the long products 5 %.
+        // Every warp goes its own way through its 32 rows.  25600 x 384 -> 1536 with GELU and z takes 53 us (the same buffers again and
+        // again) on the tiles chosen now; the forms were compared on pairs of CTAs with a shorter GELU: this one 56, lanes that store
+        // themselves (64-byte pieces of eight rows an instruction) 71, sixteen warps in teams with a buffer and barriers for each four 63
+        // to 78, and their polling costs the long products 5 %.
         const int ew = warp - 2, team = ew >> 2, lane_group = warp & 3;  // TMEM lanes [32*lane_group, +32)
         const int ncol = p.BN / 2, c_lo = team * ncol;
         uint8_t* const my_stg = stg + (size_t)ew * 2 * TL_STG;
