@@ -94,7 +94,7 @@ template <int L> __device__ __forceinline__ float ln_sum(float s, float2* red) {
 // mean is its constant (half a unit off, x - mean would be an error of 1000 * 2^-24 / sqrt(eps) in a row of 1000s).
 __device__ __forceinline__ float ln_mean(float s, float c, float inv_c) {
     const float q = s * inv_c;
-    return fmaf(fmaf(-q, c, s), inv_c, q);
+    return fabsf(q) < __int_as_float(0x7f800000) ? fmaf(fmaf(-q, c, s), inv_c, q) : q;
 }
 
 struct LnFwd {

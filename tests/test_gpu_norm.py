@@ -320,3 +320,16 @@ def test_rows_of_a_million_channels():
     _close("y", y, want, 2.0**-19 * (np.abs(want) + f(ga) * 4.0 * wrstd[:, None]))
     wdx, _, _ = ora.layer_norm_bwd(f(g), f(x), f(ga), f(mean), f(rstd))
     _close("dx", dx, wdx, 2.0**-19 * wrstd[:, None] * (2.25 + 2.25 + 2.0 * 2.25 * 2.0))
+
+
+@pytest.mark.parametrize("c", [8, 96, 999, 4096, 20000])
+def test_an_infinite_sum_is_an_infinite_mean(c):
+    import torch
+
+    from paper_2609_10632_b200 import binding as nb
+
+    x = torch.randn(3, c, device="cuda")
+    x[1, 0], x[2, c - 1] = float("inf"), float("-inf")
+    y, mean, rstd = torch.empty_like(x), torch.empty(3, device="cuda"), torch.empty(3, device="cuda")
+    nb.nb_layer_norm_fwd(0, 3, c, x, None, None, EPS, y, mean, rstd)
+    assert mean[0].isfinite() and mean[1] == float("inf") and mean[2] == float("-inf")
