@@ -6,8 +6,8 @@
  *   forward:          z = x w^T + bias;   out = act(z) + res
  *   data gradient:    dx = (dy w + add) * act_in'(z_in)      z_in [rows][c_in]: what the activation in front of this layer was given
  *   weight gradient:  dw = dy^T x;  dbias[j] = sum over the rows of dy[r][j]
- * with act one of nb_act: none, SiLU z/(1+e^-z), GELU z*Phi(z) (Phi the normal distribution function, not its tanh approximation).
- * A layer whose own activation is not followed by another layer of this kind takes nb_act_bwd for the gradient of its z.
+ * with act one of nb_act: none, SiLU z/(1+e^-z), GELU z*Phi(z) (Phi the normal distribution function, not its tanh approximation)
+ * (an infinite z has the value and the derivative of the limit).  A layer whose own activation is not followed by another layer of this kind takes nb_act_bwd for the gradient of its z.
  *
  * x, w, res, z, out, dy, add, z_in, dx are of the plan's dtype; bias, dw, dbias are fp32.  Products are accumulated in fp32 (on the
  * tensor cores, which cut off low bits, no further than a fifth of half a step of the type: longer sums leave them in between), the

@@ -11,17 +11,20 @@ namespace nbcbs {
 enum { LIN_FWD = 0, LIN_DATA = 1, LIN_WEIGHT = 2 };
 
 // ------------------------------------------------------------------------------------------ activations, fp32
+// (An infinite z has the limit's value, not the NaN of inf * 0: where z is a factor it counts as the largest finite number.  A NaN stays
+// in the other factor.)
+__device__ __forceinline__ float lin_finite(float z) { return fminf(fmaxf(z, -3.4028235e38f), 3.4028235e38f); }
 __device__ __forceinline__ float lin_act(float z, int act) {
-    if (act == NB_ACT_SILU) return z / (1.f + expf(-z));
-    if (act == NB_ACT_GELU) return 0.5f * z * erfcf(-0.70710678f * z);
+    if (act == NB_ACT_SILU) return z < 0.f ? lin_finite(z) / (1.f + expf(-z)) : z / (1.f + expf(-z));
+    if (act == NB_ACT_GELU) return z < 0.f ? 0.5f * lin_finite(z) * erfcf(-0.70710678f * z) : 0.5f * z * erfcf(-0.70710678f * z);
     return z;
 }
 __device__ __forceinline__ float lin_act_grad(float z, int act) {
     if (act == NB_ACT_SILU) {
         const float s = 1.f / (1.f + expf(-z));
-        return s * (1.f + z * (1.f - s));
+        return s * (1.f + lin_finite(z) * (1.f - s));
     }
-    if (act == NB_ACT_GELU) return fmaf(z * 0.39894228f, expf(-0.5f * z * z), 0.5f * erfcf(-0.70710678f * z));
+    if (act == NB_ACT_GELU) return fmaf(lin_finite(z) * 0.39894228f, expf(-0.5f * z * z), 0.5f * erfcf(-0.70710678f * z));
     return 1.f;
 }
 
@@ -72,7 +75,7 @@ __device__ __forceinline__ float2 lin_act2(float2 z, int act) {
         const LinTail f = lin_tail2(z);
         return fma2(mul2(f.E, f.minus_P), f.t, make_float2(fmaxf(z.x, 0.f), fmaxf(z.y, 0.f)));
     }
-    if (act == NB_ACT_SILU) return mul2(z, lin_logistic2(z));
+    if (act == NB_ACT_SILU) return mul2(make_float2(fmaxf(z.x, -3.4028235e38f), fmaxf(z.y, -3.4028235e38f)), lin_logistic2(z));
     return z;
 }
 __device__ __forceinline__ float2 lin_act_grad2(float2 z, int act) {
@@ -83,7 +86,7 @@ __device__ __forceinline__ float2 lin_act_grad2(float2 z, int act) {
     }
     if (act == NB_ACT_SILU) {
         const float2 s = lin_logistic2(z), q = fma2(s, splat2(-1.f), splat2(1.f));
-        return mul2(s, fma2(z, q, splat2(1.f)));
+        return mul2(s, fma2(make_float2(lin_finite(z.x), lin_finite(z.y)), q, splat2(1.f)));
     }
     return splat2(1.f);
 }

@@ -45,3 +45,32 @@ def test_tails_of_the_activations(n, rows, dtype, kind):
         parts = expit(hz) * (1 + t)
     off = np.abs(got - want) / (u * np.abs(want) + a * parts + np.where(hz < 0, 0.0, 2.0**-22 * (1 + t)) + tiny + 1e-30)
     assert off.max() <= 1, (off.max(), hz.reshape(-1)[off.argmax()])
+
+
+@pytest.mark.parametrize("dtype, n, rows, flags", [("bf16", 64, 128, 0), ("bf16", 64, 4, 0), ("bf16", 64, 128, 1), ("f32", 64, 128, 0), ("f32", 64, 4, 0), ("bf16", 63, 20, 0)])
+def test_infinite_arguments_have_the_limits_values(dtype, n, rows, flags):
+    """On every path: act(-inf) = 0, act(inf) = inf, act'(-inf) = 0, act'(inf) = 1; NaN stays; and the largest finite numbers likewise."""
+    import torch
+
+    from paper_2609_10632_b200 import binding as nb
+
+    dt, code = (torch.bfloat16, nb.NB_DTYPE_BF16) if dtype == "bf16" else (torch.float32, nb.NB_DTYPE_F32)
+    inf, nan = float("inf"), float("nan")
+    plan = nb.LinearPlan(n, n, code, flags=flags)
+    ws = torch.empty(plan.workspace_bytes(rows), dtype=torch.uint8, device="cuda")
+    v = torch.tensor([inf, -inf, nan, 3e38, -3e38, -200.0, 200.0, 0.0], device="cuda")
+    for act in (nb.NB_ACT_SILU, nb.NB_ACT_GELU):
+        x, w, out, dx = (torch.zeros(*s, device="cuda").to(dt) for s in ((rows, n), (n, n), (rows, n), (rows, n)))
+        x[:, 0] = 1.0
+        bias = torch.zeros(n, device="cuda")
+        bias[:8] = v
+        nb.nb_linear_fwd(plan, rows, x, w, bias, act, out, ws)
+        want = torch.tensor([inf, 0.0, nan, 3e38, 0.0, 0.0, 200.0, 0.0], device="cuda").to(dt).expand(rows, 8)
+        assert torch.equal(out[:, :8].nan_to_num(7.0, 8.0, 9.0), want.nan_to_num(7.0, 8.0, 9.0)) and out[:, 2].isnan().all(), act
+        z = torch.zeros(rows, n, device="cuda").to(dt)
+        z[:, :8] = v.to(dt)
+        w.copy_(torch.eye(n, device="cuda"))
+        for call in (lambda: nb.nb_linear_bwd_data(plan, rows, torch.ones_like(z), w, dx, ws, z_in=z, act_in=act), lambda: nb.nb_act_bwd(code, z.numel(), act, torch.ones_like(z), z, dx)):
+            call()
+            want = torch.tensor([1.0, 0.0, nan, 1.0, 0.0, 0.0, 1.0, 0.5], device="cuda").to(dt).expand(rows, 8)
+            assert torch.equal(dx[:, :8].nan_to_num(7.0), want.nan_to_num(7.0)) and dx[:, 2].isnan().all(), (act, dx[0, :8])
