@@ -25,8 +25,10 @@
  *              not zero is held as at least the smallest code (2^-9), so that it never divides as a zero.
  *              (448/largest and largest/448 are products with a reciprocal that is rounded once.)
  * A block whose largest value is below 2^-100 is held as zeros with scale 0.  A block that meets an inf or a NaN is NaN from then
- * on.  The step's own update uses m and v before they are rounded.  Every operation on the moments is rounded to fp32 by
- * itself (no fused multiply-adds), so that the codes do not depend on how a compiler contracts expressions.
+ * on.  The step's own update uses m and v before they are rounded.  Every operation of m and v is rounded to fp32 by itself (no fused
+ * multiply-adds), so that 32-bit moments do not depend on how a compiler contracts expressions.  The root that is coded and divided by is
+ * within 2^-22 of the square root of that v (a code may be its neighbour's where the root lies that close to their middle), the quotient of
+ * the update within 2^-20, and the parameter takes it in one fused multiply-add.
  *
  * All tensor pointers are DEVICE pointers on the plan's device, 16-byte aligned (scales: 4-byte); the caller owns
  * everything including the workspace.  Calls make the plan's device current while they run, enqueue on `stream` and return

@@ -64,7 +64,8 @@ nb_status nb_linear_workspace_bytes(nb_linear_plan plan, int64_t rows, size_t* b
 nb_status nb_linear_paths(nb_linear_plan plan, int64_t rows, int32_t* paths3);
 
 /* Synchronise `stream`, then report whether a kernel of this plan gave up a bounded wait (NB_ERR_TIMEOUT) or saturated an fp16 result
- * (still NB_OK; nb_last_error() says so: a loss scaler cannot see it).  Clears the status.  nb_act_bwd has no plan and counts nothing. */
+ * (still NB_OK; nb_last_error() says so: a loss scaler cannot see it; NaN counts too, and on the tensor cores parts of a row rather than
+ * elements).  Clears the status.  nb_act_bwd has no plan and counts nothing. */
 nb_status nb_linear_poll_status(nb_linear_plan plan, void* stream);
 
 /* bias, res, z may be NULL (no bias, no residual, z is not kept). */

@@ -473,7 +473,7 @@ nb_status nb_linear_poll_status(nb_linear_plan p, void* stream) {
         NB_CUDA_CHECK(cudaStreamSynchronize(st));
     }
     if (host[ST_ERR]) return fail((nb_status)host[ST_ERR], "a kernel gave up a bounded wait (site %d, block %d)", host[ST_WHERE], host[ST_DETAIL]);
-    if (host[ST_SAT]) fail(NB_OK, "%d fp16 stores of the products' results saturated", host[ST_SAT]);
+    if (host[ST_SAT]) fail(NB_OK, "%d fp16 stores of the products' results saturated or held a NaN", host[ST_SAT]);
     return NB_OK;
 }
 

@@ -389,3 +389,15 @@ def test_a_plan_keeps_its_tensors():
     plan.close()
     gc.collect()
     assert m() is None and v() is None
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_the_detectors_own_parameter_list(bits):
+    """The 243 tensors / 25.9 M parameters that the SGD step trains: filters with 16-bit copies (and 8-bit moments), two steps against the oracle."""
+    from paper_2609_10632_b200 import workloads as wl
+
+    tensors = wl.detector_parameter_tensors()
+    assert len(tensors) == 243
+    st = State([(n, group, bits if group == 0 else 32, "f32", "bf16" if group == 0 else None) for _, n, group in tensors], seed=14)
+    assert st.run(1, 0.01, 10.0) > 10.0  # clipped
+    assert st.run(2, 1e-4, 10.0) < 10.0  # not clipped
