@@ -7,6 +7,7 @@ truncate: 2^-23) and the slices in fp64: E = (K/8 + 16) * 2^-24 * S there, (K + 
       the hardware's tanh), 2.8e-4 (GELU in bf16: the same and 2.6e-5 of the fit) or 2e-5 (GELU in fp16)
   dx  |act'| E + |dy w + add| * e + u|dx|, e = 4e-5 (GELU) or 2.5e-4 (1 + |z|) (SiLU), both zero without activation
   dw, dbias  E + 2^-24 |dw|
+(a and e are bounds of earlier approximations; test_gpu_activation_tails.py holds the present ones, which are far smaller.)
 (fp32: a = e = 2^-20, some roundings of erfcf and expf.)  fp16 values below 2^-14 have steps of 2^-24: 2^-25 on top."""
 import numpy as np
 import pytest
